@@ -49,14 +49,16 @@ extern "C" {
 typedef enum {
     MXQ_OK = 0,
     MXQ_ERR_NULL = 1,      /* a required pointer is NULL */
-    MXQ_ERR_BAD_ENUM = 2,  /* dtype, scale_fmt or recipe out of range */
+    MXQ_ERR_BAD_ENUM = 2,  /* dtype, scale_fmt, elem_fmt or recipe out of range */
     MXQ_ERR_BAD_SHAPE = 3, /* n == 0, n not a multiple of block_size, block_size not in {2,4,8,16,32,64},
-                              or n so small that n/2 is not an integer */
+                              or n so small that n/2 is not an integer; 8-bit operators: rows or cols 0, a row
+                              stride below cols, block_size not in {16,32,64,128}, an output on an input with
+                              another stride */
     MXQ_ERR_ALIGN = 4,     /* a device pointer is not 16-byte aligned */
-    MXQ_ERR_BAD_SCALE = 5, /* global_scale is not finite or is <= 0 */
+    MXQ_ERR_BAD_SCALE = 5, /* global_scale or eps is not finite or is <= 0 */
     MXQ_ERR_WORKSPACE = 6, /* workspace NULL or smaller than required */
     MXQ_ERR_CUDA = 7,      /* a CUDA call failed; see mxq_last_cuda_error() */
-    MXQ_ERR_TOO_LARGE = 8  /* the size exceeds the fixed capacity of an entry point that owns its scratch */
+    MXQ_ERR_TOO_LARGE = 8  /* the size exceeds the fixed capacity of an entry point */
 } mxq_status;
 
 typedef enum { MXQ_F32 = 0, MXQ_BF16 = 1 } mxq_dtype;
@@ -294,6 +296,93 @@ int mxq_segment_mse(const float* d_block_sse, size_t n_blocks, size_t blocks_per
  *   lo, hi     0 <= lo <= hi, else MXQ_ERR_BAD_SCALE.  NaN entries pass unchanged.
  */
 int mxq_mask_interval(const void* x, int dtype, size_t n, float lo, float hi, void* d_out, void* cuda_stream);
+
+/* ---- Block-scaled 8-bit activations ------------------------------------------------------------
+ *
+ * The activations that stand between the products of a transformer block whose weights this library quantizes:
+ * an output in 8 bits in front of each product, and the same form for what the backward pass has to keep.  The paper
+ * quantizes activations to 4 bits (Results, downstream evaluation) and has no counterpart of these calls.
+ *
+ * Layout.  rows x cols elements; a block is block_size (16, 32, 64 or 128) consecutive elements of a ROW, the last
+ * one of a row may be short.
+ *   wide tensors   x, residual, dy, ...: MXQ_F32 or MXQ_BF16, rows *_stride elements apart (>= cols), elements of a row
+ *                  contiguous; aligned to their element.  Rows that start on 16 bytes and hold a multiple of 8 elements
+ *                  are read and written 16 bytes at a time, others element by element.
+ *   codes          rows * cols bytes, one element each: E4M3 (bias 7, largest 448, 0x7F and 0xFF NaN) or E5M2 (bias 15,
+ *                  largest 57344).  16-byte aligned.
+ *   scales         rows * ceil(cols / block_size) bytes, UE8M0: 2^(byte - 127); 0xFF is NaN.  Any alignment.
+ * Quantization.  The scale is the smallest power of two S >= 2^-127 with amax <= S * (largest element value): nothing is
+ * clipped.  code = RNE(v / S); the quotient is exact.  A block that holds an infinity or a NaN gets the scale byte 0xFF and
+ * codes 0x7F throughout: it reads back as NaN.  (These calls, unlike those above, take such inputs.)
+ * De-quantization.  value(code) * S in binary32, then rounded to the output's type.
+ * Arithmetic is binary32 unless said otherwise.  rows <= 2^31 - 1, at most 2^41 elements (rows padded to a multiple of
+ * 128), MXQ_ERR_TOO_LARGE beyond.  Outputs overlap neither inputs nor one another, except where a call says so.
+ */
+typedef enum { MXQ_E4M3 = 0, MXQ_E5M2 = 1 } mxq_elem_fmt;
+
+/* mxq_quantize8 -- a tensor into 8 bits, e.g. an activation checkpoint. */
+int mxq_quantize8(const void* x, int dtype, size_t rows, size_t cols, size_t x_stride, int block_size, int elem_fmt,
+                  uint8_t* out_codes, uint8_t* out_scales, void* cuda_stream);
+
+/* mxq_dequantize8 -- the way back: d_out is rows x cols of out_dtype, rows out_stride elements apart (what lies between
+ * them is left as it was). */
+int mxq_dequantize8(const uint8_t* d_codes, const uint8_t* d_scales, size_t rows, size_t cols, int block_size,
+                    int elem_fmt, void* d_out, int out_dtype, size_t out_stride, void* cuda_stream);
+
+/*
+ * mxq_add_rmsnorm8 -- residual addition and root-mean-square norm with the output in 8 bits:
+ *   h = x + residual, rounded to dtype (h = x without a residual)
+ *   rstd = 1 / sqrt(mean(h^2) + eps)          per row
+ *   y = (h * rstd) * weight                   -> out_codes, out_scales
+ *   residual, out_sum   both or neither NULL.  out_sum receives h: the next residual.  It may be x or residual itself
+ *                       (same stride), which is then updated in place.
+ *   weight              cols elements of weight_dtype (MXQ_F32 or MXQ_BF16).
+ *   kept_codes, kept_scales   both or neither NULL: h in 8 bits, for mxq_add_rmsnorm8_backward.
+ *   out_rstd            rows floats, or NULL: rstd, for the same.
+ *   eps > 0, finite.    cols <= 32768 (MXQ_ERR_TOO_LARGE beyond).
+ */
+int mxq_add_rmsnorm8(const void* x, const void* residual, const void* weight, int dtype, int weight_dtype, size_t rows,
+                     size_t cols, size_t x_stride, size_t residual_stride, float eps, int block_size, int elem_fmt,
+                     void* out_sum, size_t out_sum_stride, uint8_t* out_codes, uint8_t* out_scales, uint8_t* kept_codes,
+                     uint8_t* kept_scales, float* out_rstd, void* cuda_stream);
+
+/*
+ * mxq_add_rmsnorm8_backward -- gradients of mxq_add_rmsnorm8 from its checkpoint (rounding to 8 bits passed straight
+ * through).  With n = h * rstd, h read from kept_codes and kept_scales:
+ *   dx = rstd * (weight * dy - n * mean(weight * dy * n)) + dsum    the gradient of x and of the residual alike
+ *   dweight = sum over the rows of dy * n
+ *   dy       gradient of y.
+ *   dsum     gradient of h by its other way, the residual path, or NULL.
+ *   dx       may be dy or dsum itself (same stride).
+ *   dweight  cols floats, overwritten, or NULL: not wanted.
+ *   d_workspace  needed for dweight: mxq_add_rmsnorm8_workspace_bytes(rows, cols) bytes, 16-byte aligned; overwritten, need
+ *            not be cleared.  Calls that may run at the same time need one each.
+ * The rows are added up in an order that depends on rows, cols and the device alone: the same inputs give the same bits.
+ */
+size_t mxq_add_rmsnorm8_workspace_bytes(size_t rows, size_t cols);
+int mxq_add_rmsnorm8_backward(const void* dy, const void* dsum, const void* weight, int dtype, int weight_dtype,
+                              size_t rows, size_t cols, size_t dy_stride, size_t dsum_stride, const uint8_t* kept_codes,
+                              const uint8_t* kept_scales, const float* rstd, int block_size, int elem_fmt, void* dx,
+                              size_t dx_stride, float* dweight, void* d_workspace, size_t workspace_bytes,
+                              void* cuda_stream);
+
+/*
+ * mxq_swiglu8 -- gated activation with the output in 8 bits: a = gate / (1 + exp(-gate)) * up -> out_codes, out_scales.
+ * gate and up may be the two halves of one tensor's rows.
+ *   gate_codes, gate_scales, up_codes, up_scales   all or none NULL: gate and up in 8 bits, for mxq_swiglu8_backward.
+ */
+int mxq_swiglu8(const void* gate, const void* up, int dtype, size_t rows, size_t cols, size_t gate_stride,
+                size_t up_stride, int block_size, int elem_fmt, uint8_t* out_codes, uint8_t* out_scales,
+                uint8_t* gate_codes, uint8_t* gate_scales, uint8_t* up_codes, uint8_t* up_scales, void* cuda_stream);
+
+/*
+ * mxq_swiglu8_backward -- gradients of mxq_swiglu8 from its checkpoints, s = 1 / (1 + exp(-gate)):
+ *   dgate = dy * up * s * (1 + gate * (1 - s))       dup = dy * gate * s
+ * dgate and dup may be the two halves of one tensor's rows; one of them may be dy itself (same stride).
+ */
+int mxq_swiglu8_backward(const void* dy, int dtype, size_t rows, size_t cols, size_t dy_stride, const uint8_t* gate_codes,
+                         const uint8_t* gate_scales, const uint8_t* up_codes, const uint8_t* up_scales, int block_size,
+                         int elem_fmt, void* dgate, size_t dgate_stride, void* dup, size_t dup_stride, void* cuda_stream);
 
 /* Process-wide options, read by the entry points when they are called.
  *

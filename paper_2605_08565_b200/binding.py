@@ -26,12 +26,15 @@ LIB_PATH = os.environ.get("MXQ_LIB") or os.path.join(_HERE, "libmxq.so")
 MXQ_F32, MXQ_BF16 = 0, 1
 MXQ_SF_UE8M0, MXQ_SF_UE4M3, MXQ_SF_UE5M3 = 0, 1, 2
 MXQ_ABSMAX, MXQ_ABSMAX_PZ, MXQ_4O6, MXQ_4O6_PZ, MXQ_BRUTE, MXQ_BRUTE_PZ, MXQ_ABSMAX_OCP, MXQ_ABSMAX_CLIP7 = range(8)
+MXQ_E4M3, MXQ_E5M2 = 0, 1
 MXQ_OPT_BRUTE_PRUNE = 1
 
 EXPORTS = (
     "mxq_quantize", "mxq_quantize_ex", "mxq_quantize_mse", "mxq_quantize_batch", "mxq_fake_quantize", "mxq_tensor_amax", "mxq_global_scale_from_amax",
     "mxq_tensor_mse_workspace_bytes", "mxq_tensor_mse", "mxq_tensor_mse_static", "mxq_dequantize", "mxq_dequantize_ex",
-    "mxq_block_clip_sse", "mxq_histograms", "mxq_segment_mse", "mxq_mask_interval", "mxq_set_option", "mxq_get_option", "mxq_launch_count",
+    "mxq_block_clip_sse", "mxq_histograms", "mxq_segment_mse", "mxq_mask_interval",
+    "mxq_quantize8", "mxq_dequantize8", "mxq_add_rmsnorm8", "mxq_add_rmsnorm8_workspace_bytes", "mxq_add_rmsnorm8_backward", "mxq_swiglu8",
+    "mxq_swiglu8_backward", "mxq_set_option", "mxq_get_option", "mxq_launch_count",
     "mxq_status_string", "mxq_last_cuda_error", "mxq_version",
 )
 
@@ -110,6 +113,20 @@ def load_library() -> ctypes.CDLL:
     L.mxq_segment_mse.argtypes = [vp, sz, sz, sz, vp, vp]
     L.mxq_mask_interval.restype = i32
     L.mxq_mask_interval.argtypes = [vp, i32, sz, f32, f32, vp, vp]
+    L.mxq_quantize8.restype = i32
+    L.mxq_quantize8.argtypes = [vp, i32, sz, sz, sz, i32, i32, vp, vp, vp]
+    L.mxq_dequantize8.restype = i32
+    L.mxq_dequantize8.argtypes = [vp, vp, sz, sz, i32, i32, vp, i32, sz, vp]
+    L.mxq_add_rmsnorm8.restype = i32
+    L.mxq_add_rmsnorm8.argtypes = [vp, vp, vp, i32, i32, sz, sz, sz, sz, f32, i32, i32, vp, sz, vp, vp, vp, vp, vp, vp]
+    L.mxq_add_rmsnorm8_workspace_bytes.restype = sz
+    L.mxq_add_rmsnorm8_workspace_bytes.argtypes = [sz, sz]
+    L.mxq_add_rmsnorm8_backward.restype = i32
+    L.mxq_add_rmsnorm8_backward.argtypes = [vp, vp, vp, i32, i32, sz, sz, sz, sz, vp, vp, vp, i32, i32, vp, sz, vp, vp, sz, vp]
+    L.mxq_swiglu8.restype = i32
+    L.mxq_swiglu8.argtypes = [vp, vp, i32, sz, sz, sz, sz, i32, i32, vp, vp, vp, vp, vp, vp, vp]
+    L.mxq_swiglu8_backward.restype = i32
+    L.mxq_swiglu8_backward.argtypes = [vp, i32, sz, sz, sz, vp, vp, vp, vp, i32, i32, vp, sz, vp, sz, vp]
     L.mxq_set_option.restype = i32
     L.mxq_set_option.argtypes = [i32, i32]
     L.mxq_get_option.restype = i32
@@ -342,6 +359,174 @@ def mxq_mask_interval(x, n, lo, hi, d_out, stream=None) -> None:
     _check(load_library().mxq_mask_interval(_ptr(x), _dtype_id(x), n, lo, hi, _ptr(d_out), _stream(stream, x)))
 
 
+# ---- block-scaled 8-bit activations ---------------------------------------------------------------
+# Wide tensors are (..., cols), rows evenly spaced and elements of a row contiguous (a slice of a wider tensor's columns, say); rows, cols
+# and strides are taken from them.  Codes (uint8 or the element format's float8 type) and scales (uint8 or float8_e8m0fnu) are contiguous.
+# All tensors lie on one device, which need not be the current one.
+_CODE_TYPE = {MXQ_E4M3: torch.float8_e4m3fn, MXQ_E5M2: torch.float8_e5m2}
+
+
+class _Call8:
+    """Checks the tensors of one call against each other; the first wide tensor gives rows, cols, type and device."""
+
+    def __init__(self, first, block_size, elem_fmt):
+        if not isinstance(first, torch.Tensor) or not first.is_cuda:
+            raise MxqError("libmxq takes CUDA tensors only (no CPU fallback)")
+        if first.dim() == 0:
+            raise MxqError("a tensor of rows is expected, got a scalar")
+        if first.numel() == 0:
+            raise MxqError(f"at least one row and one element a row are expected, got {tuple(first.shape)}")
+        if isinstance(block_size, bool) or not isinstance(block_size, int) or block_size not in (16, 32, 64, 128):
+            raise MxqError(f"block_size must be 16, 32, 64 or 128, got {block_size}")
+        self.device, self.dtype, self.elem_fmt = first.device, first.dtype, elem_fmt
+        self.cols = first.shape[-1]
+        self.rows = first.numel() // self.cols
+        self.blocks = -(-self.cols // block_size)
+
+    def _on_device(self, t, what):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise MxqError("libmxq takes CUDA tensors only (no CPU fallback)")
+        if t.device != self.device:
+            raise MxqError(f"{what} lies on {t.device}, the other tensors on {self.device}")
+
+    def wide(self, t, what, optional=False):
+        """(address, row stride)"""
+        if t is None and optional:
+            return 0, 0
+        self._on_device(t, what)
+        if t.dtype != self.dtype:
+            raise MxqError(f"{what} is {t.dtype}, the other tensors {self.dtype}")
+        if t.dim() == 0 or t.shape[-1] != self.cols or t.numel() != self.rows * self.cols:
+            raise MxqError(f"{what} is {tuple(t.shape)}, {self.rows} rows of {self.cols} are expected")
+        try:
+            t = t.view(self.rows, self.cols)
+        except RuntimeError:
+            raise MxqError(f"{what}: rows must be evenly spaced") from None
+        if self.cols > 1 and t.stride(1) != 1:
+            raise MxqError(f"{what}: the elements of a row must be contiguous")
+        return t.data_ptr(), t.stride(0) if self.rows > 1 else self.cols
+
+    def held(self, codes, scales, what, optional=False):
+        if codes is None and scales is None and optional:
+            return 0, 0
+        for t, name, count, types in ((codes, what + "codes", self.rows * self.cols, (torch.uint8, _CODE_TYPE.get(self.elem_fmt))),
+                                      (scales, what + "scales", self.rows * self.blocks, (torch.uint8, torch.float8_e8m0fnu))):
+            self._on_device(t, name)
+            if t.dtype not in types:
+                raise MxqError(f"{name}: unsupported dtype {t.dtype}")
+            if not t.is_contiguous() or t.numel() != count:
+                raise MxqError(f"{name}: {count} contiguous bytes are expected, got {tuple(t.shape)}")
+        return codes.data_ptr(), scales.data_ptr()
+
+    def vector(self, t, what, count, dtype=torch.float32, optional=False):
+        if t is None and optional:
+            return 0
+        self._on_device(t, what)
+        if dtype is not None and t.dtype != dtype:
+            raise MxqError(f"{what} is {t.dtype}, {dtype} is expected")
+        if not t.is_contiguous() or t.numel() != count:
+            raise MxqError(f"{what}: {count} contiguous elements are expected, got {tuple(t.shape)}")
+        return t.data_ptr()
+
+
+def mxq_quantize8(x, block_size, elem_fmt, out_codes, out_scales, stream=None) -> None:
+    st = (_native or _load_native()).quantize8(x, block_size, elem_fmt, out_codes, out_scales, stream)
+    if st == 0:
+        return
+    if st > 0:
+        _check(st)
+    c = _Call8(x, block_size, elem_fmt)
+    (px, sx), out = c.wide(x, "x"), c.held(out_codes, out_scales, "out_")
+    with torch.cuda.device(c.device):
+        _check(load_library().mxq_quantize8(px, _dtype_id(x), c.rows, c.cols, sx, block_size, elem_fmt, *out, _stream(stream, x)))
+
+
+def mxq_dequantize8(d_codes, d_scales, block_size, elem_fmt, d_out, stream=None) -> None:
+    st = (_native or _load_native()).dequantize8(d_codes, d_scales, block_size, elem_fmt, d_out, stream)
+    if st == 0:
+        return
+    if st > 0:
+        _check(st)
+    c = _Call8(d_out, block_size, elem_fmt)
+    (po, so), held = c.wide(d_out, "d_out"), c.held(d_codes, d_scales, "d_")
+    with torch.cuda.device(c.device):
+        _check(load_library().mxq_dequantize8(*held, c.rows, c.cols, block_size, elem_fmt, po, _dtype_id(d_out), so, _stream(stream, d_out)))
+
+
+def mxq_add_rmsnorm8(x, residual, weight, eps, block_size, elem_fmt, out_sum, out_codes, out_scales, kept_codes=None, kept_scales=None,
+                     out_rstd=None, stream=None) -> None:
+    st = (_native or _load_native()).add_rmsnorm8(x, residual, weight, eps, block_size, elem_fmt, out_sum, out_codes, out_scales,
+                                                  kept_codes, kept_scales, out_rstd, stream)
+    if st == 0:
+        return
+    if st > 0:
+        _check(st)
+    c = _Call8(x, block_size, elem_fmt)
+    (px, sx), (pr, sr), (ps, ss) = c.wide(x, "x"), c.wide(residual, "residual", True), c.wide(out_sum, "out_sum", True)
+    pw = c.vector(weight, "weight", c.cols, None)
+    out, kept = c.held(out_codes, out_scales, "out_"), c.held(kept_codes, kept_scales, "kept_", True)
+    rstd = c.vector(out_rstd, "out_rstd", c.rows, optional=True)
+    with torch.cuda.device(c.device):
+        _check(load_library().mxq_add_rmsnorm8(px, pr, pw, _dtype_id(x), _dtype_id(weight), c.rows, c.cols, sx, sr, eps, block_size, elem_fmt,
+                                               ps, ss, *out, *kept, rstd, _stream(stream, x)))
+
+
+def mxq_add_rmsnorm8_workspace_bytes(rows: int, cols: int) -> int:
+    return int(load_library().mxq_add_rmsnorm8_workspace_bytes(rows, cols))
+
+
+def mxq_add_rmsnorm8_backward(dy, dsum, weight, kept_codes, kept_scales, rstd, block_size, elem_fmt, dx, dweight=None, d_workspace=None,
+                              stream=None) -> None:
+    st = (_native or _load_native()).add_rmsnorm8_backward(dy, dsum, weight, kept_codes, kept_scales, rstd, block_size, elem_fmt, dx, dweight,
+                                                           d_workspace, stream)
+    if st == 0:
+        return
+    if st > 0:
+        _check(st)
+    c = _Call8(dy, block_size, elem_fmt)
+    (py, sy), (ps, ss), (px, sx) = c.wide(dy, "dy"), c.wide(dsum, "dsum", True), c.wide(dx, "dx")
+    pw = c.vector(weight, "weight", c.cols, None)
+    kept, prs = c.held(kept_codes, kept_scales, "kept_"), c.vector(rstd, "rstd", c.rows)
+    pdw = c.vector(dweight, "dweight", c.cols, optional=True)
+    pws = c.vector(d_workspace, "d_workspace", d_workspace.numel(), None) if d_workspace is not None else 0
+    ws_bytes = d_workspace.numel() * d_workspace.element_size() if d_workspace is not None else 0
+    with torch.cuda.device(c.device):
+        _check(load_library().mxq_add_rmsnorm8_backward(py, ps, pw, _dtype_id(dy), _dtype_id(weight), c.rows, c.cols, sy, ss, *kept, prs,
+                                                        block_size, elem_fmt, px, sx, pdw, pws, ws_bytes, _stream(stream, dy)))
+
+
+def mxq_swiglu8(gate, up, block_size, elem_fmt, out_codes, out_scales, gate_codes=None, gate_scales=None, up_codes=None, up_scales=None,
+                stream=None) -> None:
+    st = (_native or _load_native()).swiglu8(gate, up, block_size, elem_fmt, out_codes, out_scales, gate_codes, gate_scales, up_codes,
+                                             up_scales, stream)
+    if st == 0:
+        return
+    if st > 0:
+        _check(st)
+    c = _Call8(gate, block_size, elem_fmt)
+    (pg, sg), (pu, su) = c.wide(gate, "gate"), c.wide(up, "up")
+    out = c.held(out_codes, out_scales, "out_")
+    kept = (*c.held(gate_codes, gate_scales, "gate_", True), *c.held(up_codes, up_scales, "up_", True))
+    with torch.cuda.device(c.device):
+        _check(load_library().mxq_swiglu8(pg, pu, _dtype_id(gate), c.rows, c.cols, sg, su, block_size, elem_fmt, *out, *kept,
+                                          _stream(stream, gate)))
+
+
+def mxq_swiglu8_backward(dy, gate_codes, gate_scales, up_codes, up_scales, block_size, elem_fmt, dgate, dup, stream=None) -> None:
+    st = (_native or _load_native()).swiglu8_backward(dy, gate_codes, gate_scales, up_codes, up_scales, block_size, elem_fmt, dgate, dup,
+                                                      stream)
+    if st == 0:
+        return
+    if st > 0:
+        _check(st)
+    c = _Call8(dy, block_size, elem_fmt)
+    (py, sy), (pg, sg), (pu, su) = c.wide(dy, "dy"), c.wide(dgate, "dgate"), c.wide(dup, "dup")
+    kept = (*c.held(gate_codes, gate_scales, "gate_"), *c.held(up_codes, up_scales, "up_"))
+    with torch.cuda.device(c.device):
+        _check(load_library().mxq_swiglu8_backward(py, _dtype_id(dy), c.rows, c.cols, sy, *kept, block_size, elem_fmt, pg, sg, pu, su,
+                                                   _stream(stream, dy)))
+
+
 def mxq_set_option(option: int, value: int) -> None:
     st = (_native or _load_native()).set_option(int(option), int(value))
     if st == 0:
@@ -389,3 +574,18 @@ def tensor_mse(block_sse: torch.Tensor, n: int, stream=None) -> torch.Tensor:
     out = torch.empty(1, dtype=torch.float64, device=block_sse.device)
     mxq_tensor_mse(block_sse, block_sse.numel(), n, out, ws, stream)
     return out
+
+
+def alloc_outputs8(rows: int, cols: int, block_size: int, elem_fmt: int, device):
+    """Codes and scales of one 8-bit tensor, as the float8 types that torch has for them."""
+    codes = torch.empty(rows, cols, dtype=_CODE_TYPE[elem_fmt], device=device)
+    scales = torch.empty(rows, -(-cols // block_size), dtype=torch.float8_e8m0fnu, device=device)
+    return codes, scales
+
+
+def quantize8(x: torch.Tensor, block_size: int = 32, elem_fmt: int = MXQ_E4M3, stream=None):
+    """Allocates (codes, scales) and runs mxq_quantize8 on the rows of x."""
+    cols = x.shape[-1]
+    codes, scales = alloc_outputs8(x.numel() // cols if cols else 0, cols, block_size, elem_fmt, x.device)
+    mxq_quantize8(x, block_size, elem_fmt, codes, scales, stream)
+    return codes, scales

@@ -32,6 +32,8 @@ static int cuda_fail(cudaError_t e) {
 }
 
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+static bool aligned_elem(const void* p, int dtype) { return (reinterpret_cast<uintptr_t>(p) & (dtype == MXQ_F32 ? 3u : 1u)) == 0; }
+static bool valid_block8(int b) { return b == 16 || b == 32 || b == 64 || b == 128; }
 static bool valid_block(int b) { return b == 2 || b == 4 || b == 8 || b == 16 || b == 32 || b == 64; }
 
 }  // namespace mxq
@@ -300,6 +302,130 @@ int mxq_mask_interval(const void* x, int dtype, size_t n, float lo, float hi, vo
     return err == cudaSuccess ? MXQ_OK : cuda_fail(err);
 }
 
+// Shared by the operators on 8-bit activations: types, block size and shape.
+static int check8(size_t rows, size_t cols, int dtype, int block_size, int elem_fmt) {
+    if (dtype != MXQ_F32 && dtype != MXQ_BF16) return MXQ_ERR_BAD_ENUM;
+    if (elem_fmt != MXQ_E4M3 && elem_fmt != MXQ_E5M2) return MXQ_ERR_BAD_ENUM;
+    if (!valid_block8(block_size) || rows == 0 || cols == 0) return MXQ_ERR_BAD_SHAPE;
+    if (rows > kAct8MaxRows || cols > kAct8MaxElems || rows * ((cols + 127) / 128 * 128) > kAct8MaxElems) return MXQ_ERR_TOO_LARGE;
+    return MXQ_OK;
+}
+// A tensor whose rows lie `stride` elements apart.
+static int check_wide(const void* p, size_t stride, size_t cols, int dtype) {
+    if (!p) return MXQ_ERR_NULL;
+    if (stride < cols) return MXQ_ERR_BAD_SHAPE;
+    return aligned_elem(p, dtype) ? MXQ_OK : MXQ_ERR_ALIGN;
+}
+static int check_held(const uint8_t* codes, const uint8_t* scales) {
+    if (!codes || !scales) return MXQ_ERR_NULL;
+    return aligned16(codes) ? MXQ_OK : MXQ_ERR_ALIGN;
+}
+// One tensor written where another is read is right only element for element.
+static bool in_step(const void* out, size_t out_stride, const void* in, size_t in_stride, size_t rows) { return out != in || out_stride == in_stride || rows == 1; }
+static Wide8 wide(const void* p, size_t stride) { return {const_cast<void*>(p), stride}; }
+static Held8 held(const uint8_t* codes, const uint8_t* scales) { return {const_cast<uint8_t*>(codes), const_cast<uint8_t*>(scales)}; }
+#define MXQ_TRY(expr)                        \
+    do {                                     \
+        const int st_ = (expr);              \
+        if (st_ != MXQ_OK) return st_;       \
+    } while (0)
+
+int mxq_quantize8(const void* x, int dtype, size_t rows, size_t cols, size_t x_stride, int block_size, int elem_fmt, uint8_t* out_codes, uint8_t* out_scales,
+                  void* cuda_stream) {
+    MXQ_TRY(check8(rows, cols, dtype, block_size, elem_fmt));
+    MXQ_TRY(check_wide(x, x_stride, cols, dtype));
+    MXQ_TRY(check_held(out_codes, out_scales));
+    cudaError_t err = launch_quantize8(wide(x, x_stride), rows, cols, block_size, dtype, elem_fmt, held(out_codes, out_scales), static_cast<cudaStream_t>(cuda_stream));
+    return err == cudaSuccess ? MXQ_OK : cuda_fail(err);
+}
+
+int mxq_dequantize8(const uint8_t* d_codes, const uint8_t* d_scales, size_t rows, size_t cols, int block_size, int elem_fmt, void* d_out, int out_dtype, size_t out_stride,
+                    void* cuda_stream) {
+    MXQ_TRY(check8(rows, cols, out_dtype, block_size, elem_fmt));
+    MXQ_TRY(check_held(d_codes, d_scales));
+    MXQ_TRY(check_wide(d_out, out_stride, cols, out_dtype));
+    cudaError_t err = launch_dequantize8(held(d_codes, d_scales), rows, cols, block_size, out_dtype, elem_fmt, wide(d_out, out_stride), static_cast<cudaStream_t>(cuda_stream));
+    return err == cudaSuccess ? MXQ_OK : cuda_fail(err);
+}
+
+int mxq_add_rmsnorm8(const void* x, const void* residual, const void* weight, int dtype, int weight_dtype, size_t rows, size_t cols, size_t x_stride, size_t residual_stride,
+                     float eps, int block_size, int elem_fmt, void* out_sum, size_t out_sum_stride, uint8_t* out_codes, uint8_t* out_scales, uint8_t* kept_codes,
+                     uint8_t* kept_scales, float* out_rstd, void* cuda_stream) {
+    MXQ_TRY(check8(rows, cols, dtype, block_size, elem_fmt));
+    if (weight_dtype != MXQ_F32 && weight_dtype != MXQ_BF16) return MXQ_ERR_BAD_ENUM;
+    if (cols > kNorm8MaxCols) return MXQ_ERR_TOO_LARGE;
+    if (!(eps > 0.0f && std::isfinite(eps))) return MXQ_ERR_BAD_SCALE;
+    MXQ_TRY(check_wide(x, x_stride, cols, dtype));
+    if (!weight || !residual != !out_sum || !kept_codes != !kept_scales) return MXQ_ERR_NULL;
+    if (residual) {
+        MXQ_TRY(check_wide(residual, residual_stride, cols, dtype));
+        MXQ_TRY(check_wide(out_sum, out_sum_stride, cols, dtype));
+        if (!in_step(out_sum, out_sum_stride, x, x_stride, rows) || !in_step(out_sum, out_sum_stride, residual, residual_stride, rows)) return MXQ_ERR_BAD_SHAPE;
+    }
+    MXQ_TRY(check_held(out_codes, out_scales));
+    if (kept_codes) MXQ_TRY(check_held(kept_codes, kept_scales));
+    if (!aligned_elem(weight, weight_dtype) || !aligned_elem(out_rstd, MXQ_F32)) return MXQ_ERR_ALIGN;
+    cudaError_t err = launch_add_rmsnorm8(wide(x, x_stride), wide(residual, residual_stride), weight, weight_dtype, rows, cols, eps, block_size, dtype, elem_fmt,
+                                          wide(out_sum, out_sum_stride), held(out_codes, out_scales), held(kept_codes, kept_scales), out_rstd,
+                                          static_cast<cudaStream_t>(cuda_stream));
+    return err == cudaSuccess ? MXQ_OK : cuda_fail(err);
+}
+
+size_t mxq_add_rmsnorm8_workspace_bytes(size_t rows, size_t cols) {
+    return (rows < (size_t)kNorm8Parts ? rows : (size_t)kNorm8Parts) * (cols < kNorm8MaxCols ? cols : kNorm8MaxCols) * sizeof(float);
+}
+
+int mxq_add_rmsnorm8_backward(const void* dy, const void* dsum, const void* weight, int dtype, int weight_dtype, size_t rows, size_t cols, size_t dy_stride, size_t dsum_stride,
+                              const uint8_t* kept_codes, const uint8_t* kept_scales, const float* rstd, int block_size, int elem_fmt, void* dx, size_t dx_stride,
+                              float* dweight, void* d_workspace, size_t workspace_bytes, void* cuda_stream) {
+    MXQ_TRY(check8(rows, cols, dtype, block_size, elem_fmt));
+    if (weight_dtype != MXQ_F32 && weight_dtype != MXQ_BF16) return MXQ_ERR_BAD_ENUM;
+    if (cols > kNorm8MaxCols) return MXQ_ERR_TOO_LARGE;
+    MXQ_TRY(check_wide(dy, dy_stride, cols, dtype));
+    if (dsum) MXQ_TRY(check_wide(dsum, dsum_stride, cols, dtype));
+    if (!weight || !rstd) return MXQ_ERR_NULL;
+    MXQ_TRY(check_held(kept_codes, kept_scales));
+    MXQ_TRY(check_wide(dx, dx_stride, cols, dtype));
+    if (!in_step(dx, dx_stride, dy, dy_stride, rows) || !in_step(dx, dx_stride, dsum, dsum_stride, rows)) return MXQ_ERR_BAD_SHAPE;
+    if (!aligned_elem(weight, weight_dtype) || !aligned_elem(rstd, MXQ_F32) || !aligned_elem(dweight, MXQ_F32)) return MXQ_ERR_ALIGN;
+    if (dweight) {
+        if (!d_workspace || workspace_bytes < mxq_add_rmsnorm8_workspace_bytes(rows, cols)) return MXQ_ERR_WORKSPACE;
+        if (!aligned16(d_workspace)) return MXQ_ERR_ALIGN;
+    }
+    cudaError_t err = launch_add_rmsnorm8_backward(wide(dy, dy_stride), wide(dsum, dsum_stride), weight, weight_dtype, held(kept_codes, kept_scales), rstd, rows, cols, block_size,
+                                                   dtype, elem_fmt, wide(dx, dx_stride), dweight, static_cast<float*>(d_workspace), static_cast<cudaStream_t>(cuda_stream));
+    return err == cudaSuccess ? MXQ_OK : cuda_fail(err);
+}
+
+int mxq_swiglu8(const void* gate, const void* up, int dtype, size_t rows, size_t cols, size_t gate_stride, size_t up_stride, int block_size, int elem_fmt, uint8_t* out_codes,
+                uint8_t* out_scales, uint8_t* gate_codes, uint8_t* gate_scales, uint8_t* up_codes, uint8_t* up_scales, void* cuda_stream) {
+    MXQ_TRY(check8(rows, cols, dtype, block_size, elem_fmt));
+    MXQ_TRY(check_wide(gate, gate_stride, cols, dtype));
+    MXQ_TRY(check_wide(up, up_stride, cols, dtype));
+    MXQ_TRY(check_held(out_codes, out_scales));
+    if (gate_codes || gate_scales || up_codes || up_scales) {
+        MXQ_TRY(check_held(gate_codes, gate_scales));
+        MXQ_TRY(check_held(up_codes, up_scales));
+    }
+    cudaError_t err = launch_swiglu8(wide(gate, gate_stride), wide(up, up_stride), rows, cols, block_size, dtype, elem_fmt, held(out_codes, out_scales),
+                                     held(gate_codes, gate_scales), held(up_codes, up_scales), static_cast<cudaStream_t>(cuda_stream));
+    return err == cudaSuccess ? MXQ_OK : cuda_fail(err);
+}
+
+int mxq_swiglu8_backward(const void* dy, int dtype, size_t rows, size_t cols, size_t dy_stride, const uint8_t* gate_codes, const uint8_t* gate_scales, const uint8_t* up_codes,
+                         const uint8_t* up_scales, int block_size, int elem_fmt, void* dgate, size_t dgate_stride, void* dup, size_t dup_stride, void* cuda_stream) {
+    MXQ_TRY(check8(rows, cols, dtype, block_size, elem_fmt));
+    MXQ_TRY(check_wide(dy, dy_stride, cols, dtype));
+    MXQ_TRY(check_held(gate_codes, gate_scales));
+    MXQ_TRY(check_held(up_codes, up_scales));
+    MXQ_TRY(check_wide(dgate, dgate_stride, cols, dtype));
+    MXQ_TRY(check_wide(dup, dup_stride, cols, dtype));
+    if (dgate == dup || !in_step(dgate, dgate_stride, dy, dy_stride, rows) || !in_step(dup, dup_stride, dy, dy_stride, rows)) return MXQ_ERR_BAD_SHAPE;
+    cudaError_t err = launch_swiglu8_backward(wide(dy, dy_stride), held(gate_codes, gate_scales), held(up_codes, up_scales), rows, cols, block_size, dtype, elem_fmt,
+                                              wide(dgate, dgate_stride), wide(dup, dup_stride), static_cast<cudaStream_t>(cuda_stream));
+    return err == cudaSuccess ? MXQ_OK : cuda_fail(err);
+}
+
 int mxq_set_option(int option, int value) {
     if (option != MXQ_OPT_BRUTE_PRUNE || (value != 0 && value != 1)) return MXQ_ERR_BAD_ENUM;
     g_brute_prune.store(value, std::memory_order_relaxed);
@@ -319,10 +445,10 @@ const char* mxq_status_string(int status) {
     switch (status) {
     case MXQ_OK: return "ok";
     case MXQ_ERR_NULL: return "a required pointer is NULL";
-    case MXQ_ERR_BAD_ENUM: return "dtype, scale format or recipe out of range";
-    case MXQ_ERR_BAD_SHAPE: return "n must be a positive multiple of block_size, block_size in {2,4,8,16,32,64}";
+    case MXQ_ERR_BAD_ENUM: return "dtype, scale format, element format or recipe out of range";
+    case MXQ_ERR_BAD_SHAPE: return "n must be a positive multiple of block_size, block_size in {2,4,8,16,32,64} (8-bit operators: rows, cols >= 1, strides >= cols, block_size in {16,32,64,128})";
     case MXQ_ERR_ALIGN: return "device pointer not sufficiently aligned";
-    case MXQ_ERR_BAD_SCALE: return "global_scale must be finite and > 0";
+    case MXQ_ERR_BAD_SCALE: return "global_scale or eps must be finite and > 0";
     case MXQ_ERR_WORKSPACE: return "workspace missing or too small";
     case MXQ_ERR_CUDA: return "CUDA call failed (see mxq_last_cuda_error)";
     case MXQ_ERR_TOO_LARGE: return "size exceeds the fixed capacity of this entry point (use the workspace variant)";

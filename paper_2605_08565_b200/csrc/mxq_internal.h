@@ -125,4 +125,35 @@ constexpr int kMsePartials = 1024;  // fixed first-level width of the MSE tree
 // Second level of the tensor-MSE tree alone: out = (sum of n_partials <= kMsePartials partials) / n.
 cudaError_t launch_mse_final(const double* d_partials, int n_partials, size_t n, double* d_out, cudaStream_t s);
 
+// ---- operators on block-scaled 8-bit activations (mxq_act8.cu, mxq_norm8.cu) ----
+// An 8-bit tensor of contiguous rows: codes rows x cols, scales rows x blocks; both NULL: not there.
+struct Held8 {
+    uint8_t* codes;
+    uint8_t* scales;
+};
+// A bf16 or fp32 tensor whose rows lie `stride` elements apart; p NULL: not there.
+struct Wide8 {
+    void* p;
+    size_t stride;
+};
+// Whether its rows can be read and written 16 bytes at a time, in whole vectors of 8 elements.
+inline bool wide_vec(const Wide8& w, size_t cols, int dtype) {
+    return (reinterpret_cast<uintptr_t>(w.p) & 15u) == 0 && cols % 8 == 0 && w.stride % (dtype == 0 ? 4 : 8) == 0;
+}
+constexpr size_t kAct8MaxRows = 0x7FFFFFFF;          // a grid's limit
+constexpr size_t kAct8MaxElems = (size_t)1 << 41;    // rows padded to 128 elements
+constexpr int kNorm8Parts = 1024;         // rows of partial sums in the workspace of the norm's gradient
+constexpr size_t kNorm8MaxCols = 32768;   // elements of a row that a CTA of the norms can hold
+
+cudaError_t launch_quantize8(const Wide8& x, size_t rows, size_t cols, int B, int dtype, int fmt, const Held8& out, cudaStream_t s);
+cudaError_t launch_dequantize8(const Held8& in, size_t rows, size_t cols, int B, int dtype, int fmt, const Wide8& out, cudaStream_t s);
+cudaError_t launch_swiglu8(const Wide8& gate, const Wide8& up, size_t rows, size_t cols, int B, int dtype, int fmt, const Held8& out, const Held8& out_gate,
+                           const Held8& out_up, cudaStream_t s);
+cudaError_t launch_swiglu8_backward(const Wide8& dy, const Held8& gate, const Held8& up, size_t rows, size_t cols, int B, int dtype, int fmt, const Wide8& dgate,
+                                    const Wide8& dup, cudaStream_t s);
+cudaError_t launch_add_rmsnorm8(const Wide8& x, const Wide8& residual, const void* weight, int weight_dtype, size_t rows, size_t cols, float eps, int B, int dtype, int fmt,
+                                const Wide8& out_sum, const Held8& out, const Held8& kept, float* out_rstd, cudaStream_t s);
+cudaError_t launch_add_rmsnorm8_backward(const Wide8& dy, const Wide8& dsum, const void* weight, int weight_dtype, const Held8& kept, const float* rstd, size_t rows, size_t cols,
+                                         int B, int dtype, int fmt, const Wide8& dx, float* dweight, float* parts, cudaStream_t s);
+
 }  // namespace mxq
