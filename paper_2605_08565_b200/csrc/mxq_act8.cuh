@@ -1,9 +1,14 @@
 // Device-side building blocks of the operators on block-scaled 8-bit activations: rows of E4M3 or E5M2 elements with one
 // power-of-two scale byte (UE8M0) per block of B = 16, 32, 64 or 128 consecutive elements of a row.
 //
-// A thread works on vectors of 8 consecutive elements (16 bytes of bf16, 32 of fp32, 8 code bytes), so a block lies in B / 8
-// neighbouring lanes of one warp and its maximum takes log2(B / 8) shuffles.  Rows are padded to whole blocks in this numbering: the
-// lanes behind the end of a row hold zeros and store nothing.
+// A thread works on vectors of 32 bytes of a wide tensor: 16 bf16 or 8 fp32 elements, 16 or 8 code bytes.  A block lies in
+// B / 16 or B / 8 neighbouring lanes of one warp, and its maximum takes at most four shuffles.  Rows are padded to whole blocks in
+// this numbering: the lanes behind the end of a row hold zeros and store nothing.
+//
+// Rows that start on 32 bytes and hold whole vectors (VEC) are read and written one vector at a time.  Any other row (an odd number of
+// elements, a view that starts anywhere) is read in the aligned 16-byte pieces that its bytes lie in, shifted into place in
+// registers; on the way out neighbouring lanes exchange what belongs into the other's aligned pieces, and only the two ends of a warp's
+// run are stored element by element.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -16,107 +21,189 @@
 namespace mxq {
 
 constexpr int kE4M3 = 0, kE5M2 = 1;
-constexpr int kVec = 8;   // elements of a vector
+constexpr unsigned kFull = 0xFFFFFFFFu;
+// Elements of a vector.
+__host__ __device__ constexpr int vec_elems(int dt) { return dt == kF32 ? 8 : 16; }
 
-// ---- vectors of 8 elements as fp32 ---------------------------------------------------------------
-// VEC: the caller has checked that rows start on 16 bytes and hold whole vectors.  Otherwise element by element, `left` (<= 0: none)
-// of them; the rest are zeros.
-template <int DT, bool VEC>
-__device__ __forceinline__ void load8(const void* base, size_t at, int left, float (&v)[kVec]) {
+// ---- bytes ---------------------------------------------------------------------------------------
+// w = the words of c from byte `by` (< 4 * (M - N)) on.
+template <int N, int M>
+__device__ __forceinline__ void shift_down(uint32_t (&c)[M], unsigned by, uint32_t (&w)[N]) {
+    if constexpr (M - N > 2) {
+#pragma unroll
+        for (int i = 0; i + 2 < M; ++i) c[i] = by & 8u ? c[i + 2] : c[i];
+    }
+#pragma unroll
+    for (int i = 0; i + 1 < M; ++i) c[i] = by & 4u ? c[i + 1] : c[i];
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = __funnelshift_r(c[i], c[i + 1 < M ? i + 1 : i], 8u * (by & 3u));
+}
+
+__device__ __forceinline__ void load256(const void* p, uint32_t* w) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                 : "l"(p)
+                 : "memory");
+}
+__device__ __forceinline__ void store256(void* p, const uint32_t* w) {
+    asm volatile("st.global.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]),
+                 "l"(p)
+                 : "memory");
+}
+
+// NB bytes from p on, of which the first `valid` exist (the others become zeros).  Without VEC the aligned pieces are read whole: a
+// piece that holds a byte of the row is mapped as a whole.
+template <int NB, bool VEC>
+__device__ __forceinline__ void load_bytes(const void* p, int valid, uint32_t (&w)[NB / 4]) {
+    constexpr int N = NB / 4;
     if constexpr (VEC) {
-        if (left <= 0) {
 #pragma unroll
-            for (int j = 0; j < kVec; ++j) v[j] = 0.0f;
-            return;
-        }
-        if constexpr (DT == kBF16) {
-            const uint4 w = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + at);
-            const uint32_t p[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v[2 * j] = __uint_as_float(p[j] << 16);
-                v[2 * j + 1] = __uint_as_float(p[j] & 0xFFFF0000u);
-            }
+        for (int i = 0; i < N; ++i) w[i] = 0u;
+        if (valid <= 0) return;
+        if constexpr (NB == 8) {
+            const uint2 a = *static_cast<const uint2*>(p);
+            w[0] = a.x, w[1] = a.y;
+        } else if constexpr (NB == 16) {
+            const uint4 a = *static_cast<const uint4*>(p);
+            w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
         } else {
-            const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(base) + at);
-            const float4 a = q[0], b = q[1];
-            v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+#pragma unroll
+            for (int i = 0; i < N; i += 8) load256(static_cast<const char*>(p) + 4 * i, w + i);
         }
     } else {
+        constexpr int G = NB < 16 ? NB : 16, M = N + G / 4;
+        const unsigned by = (unsigned)(reinterpret_cast<uintptr_t>(p) & (G - 1));
+        const char* q = static_cast<const char*>(p) - by;
+        uint32_t c[M];
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) {
-            v[j] = 0.0f;
-            if (j < left) {
-                if constexpr (DT == kBF16) v[j] = __uint_as_float((uint32_t) static_cast<const uint16_t*>(base)[at + j] << 16);
-                else v[j] = static_cast<const float*>(base)[at + j];
+        for (int i = 0; i < M; ++i) c[i] = 0u;
+#pragma unroll
+        for (int i = 0; i < M * 4 / G; ++i) {
+            if (valid > 0 && i * G < (int)by + valid) {
+                if constexpr (G == 16) {
+                    const uint4 a = *reinterpret_cast<const uint4*>(q + i * G);
+                    c[4 * i] = a.x, c[4 * i + 1] = a.y, c[4 * i + 2] = a.z, c[4 * i + 3] = a.w;
+                } else {
+                    const uint2 a = *reinterpret_cast<const uint2*>(q + i * G);
+                    c[2 * i] = a.x, c[2 * i + 1] = a.y;
+                }
+            }
+        }
+        shift_down<N, M>(c, by, w);
+        if (valid < NB) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int n = valid - 4 * i;
+                w[i] = n >= 4 ? w[i] : n <= 0 ? 0u : w[i] & (0xFFFFFFFFu >> (32 - 8 * n));
             }
         }
     }
 }
 
-// Rounds to bf16 (to nearest even) where the type asks for it: bits of two elements in a word, the first in the low half.
+// NB bytes to p on, of which the first `valid` are stored, in elements of EB bytes.  A warp's lanes hold consecutive vectors, of one row
+// or of several: `first` tells that a vector starts its row, and `after` counts the bytes that its row holds behind it.  All 32 lanes call it.
+template <int NB, int EB, bool VEC>
+__device__ __forceinline__ void store_bytes(void* p, int valid, bool first, long long after, const uint32_t (&w)[NB / 4]) {
+    constexpr int N = NB / 4;
+    if constexpr (VEC) {
+        if (valid <= 0) return;
+        if constexpr (NB == 8) {
+            *static_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+        } else if constexpr (NB == 16) {
+            *static_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; i += 8) store256(static_cast<char*>(p) + 4 * i, w + i);
+        }
+    } else {
+        constexpr int G = NB < 16 ? NB : 16, GW = G / 4, C = NB / G;
+        const unsigned lane = threadIdx.x & 31;
+        const int h = (int)((0u - (unsigned)reinterpret_cast<uintptr_t>(p)) & (G - 1));   // bytes in front of the first aligned piece
+        uint32_t c[N + GW];
+#pragma unroll
+        for (int i = 0; i < N; ++i) c[i] = w[i];
+#pragma unroll
+        for (int i = 0; i < GW; ++i) c[N + i] = __shfl_down_sync(kFull, w[i], 1);
+        uint32_t out[N];
+        shift_down<N, N + GW>(c, (unsigned)h, out);
+        if (valid <= 0) return;
+        const bool head_taken = h == 0 || (lane > 0 && !first && valid >= h);   // by the lane before
+        const bool last_whole = valid == NB && (h == 0 || (lane < 31 && after >= h));
+        char* q = static_cast<char*>(p) + h;
+        int done = h;   // bytes in front of which everything but an untaken head is stored
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            if (i + 1 < C ? h + (i + 1) * G <= valid : last_whole) {
+                if constexpr (G == 16) *reinterpret_cast<uint4*>(q + i * G) = make_uint4(out[4 * i], out[4 * i + 1], out[4 * i + 2], out[4 * i + 3]);
+                else *reinterpret_cast<uint2*>(q + i * G) = make_uint2(out[2 * i], out[2 * i + 1]);
+                done += G;
+            }
+        }
+        if (!head_taken || done < valid) {
+#pragma unroll
+            for (int b = 0; b < NB; b += EB) {
+                if (b < valid && (b >= done || (b < h && !head_taken))) {
+                    char* to = static_cast<char*>(p) + b;
+                    if constexpr (EB == 4) *reinterpret_cast<uint32_t*>(to) = w[b / 4];
+                    else if constexpr (EB == 2) *reinterpret_cast<uint16_t*>(to) = (uint16_t)(w[b / 4] >> (8 * (b & 3)));
+                    else *reinterpret_cast<uint8_t*>(to) = (uint8_t)(w[b / 4] >> (8 * (b & 3)));
+                }
+            }
+        }
+    }
+}
+
+// ---- values --------------------------------------------------------------------------------------
+// Rounds two values to bf16 (to nearest even): a in the low half of the word.
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
     return r;
 }
 
-template <int DT, bool VEC>
-__device__ __forceinline__ void store8(void* base, size_t at, int left, const float (&v)[kVec]) {
-    if constexpr (VEC) {
-        if (left <= 0) return;
-        if constexpr (DT == kBF16) {
-            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(base) + at) =
-                make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-        } else {
-            float4* q = reinterpret_cast<float4*>(static_cast<float*>(base) + at);
-            q[0] = make_float4(v[0], v[1], v[2], v[3]);
-            q[1] = make_float4(v[4], v[5], v[6], v[7]);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < kVec; ++j) {
-            if (j < left) {
-                if constexpr (DT == kBF16) static_cast<uint16_t*>(base)[at + j] = (uint16_t)pack_bf16(v[j], 0.0f);
-                else static_cast<float*>(base)[at + j] = v[j];
-            }
-        }
-    }
-}
-
-// What a value becomes when it is stored as DT and read back.
-template <int DT>
-__device__ __forceinline__ void round8(float (&v)[kVec]) {
+template <int DT, int V>
+__device__ __forceinline__ void unpack(const uint32_t* w, float (&v)[V]) {
     if constexpr (DT == kBF16) {
 #pragma unroll
-        for (int j = 0; j < kVec; j += 2) {
-            const uint32_t p = pack_bf16(v[j], v[j + 1]);
-            v[j] = __uint_as_float(p << 16);
-            v[j + 1] = __uint_as_float(p & 0xFFFF0000u);
+        for (int j = 0; j < V; j += 2) {
+            v[j] = __uint_as_float(w[j / 2] << 16);
+            v[j + 1] = __uint_as_float(w[j / 2] & 0xFFFF0000u);
         }
-    }
-}
-
-template <bool VEC>
-__device__ __forceinline__ uint2 load_codes8(const uint8_t* base, size_t at, int left) {
-    if constexpr (VEC) return left > 0 ? *reinterpret_cast<const uint2*>(base + at) : make_uint2(0u, 0u);
-    uint32_t w[2] = {0u, 0u};
-#pragma unroll
-    for (int j = 0; j < kVec; ++j)
-        if (j < left) w[j >> 2] |= (uint32_t)base[at + j] << (8 * (j & 3));
-    return make_uint2(w[0], w[1]);
-}
-
-template <bool VEC>
-__device__ __forceinline__ void store_codes8(uint8_t* base, size_t at, int left, uint2 c) {
-    if constexpr (VEC) {
-        if (left > 0) *reinterpret_cast<uint2*>(base + at) = c;
     } else {
-        const uint32_t w[2] = {c.x, c.y};
 #pragma unroll
-        for (int j = 0; j < kVec; ++j)
-            if (j < left) base[at + j] = (uint8_t)(w[j >> 2] >> (8 * (j & 3)));
+        for (int j = 0; j < V; ++j) v[j] = __uint_as_float(w[j]);
     }
+}
+template <int DT, int V>
+__device__ __forceinline__ void pack(const float (&v)[V], uint32_t* w) {
+    if constexpr (DT == kBF16) {
+#pragma unroll
+        for (int j = 0; j < V; j += 2) w[j / 2] = pack_bf16(v[j], v[j + 1]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) w[j] = __float_as_uint(v[j]);
+    }
+}
+
+// Two binary32 products in one instruction, each rounded to nearest even.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    uint64_t x, y, z;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a.x), "f"(a.y));
+    asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(b.x), "f"(b.y));
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(z) : "l"(x), "l"(y));
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(z));
+    return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    uint64_t x, y, t, z;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a.x), "f"(a.y));
+    asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(b.x), "f"(b.y));
+    asm("mov.b64 %0, {%1, %2};" : "=l"(t) : "f"(c.x), "f"(c.y));
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(z) : "l"(x), "l"(y), "l"(t));
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(z));
+    return r;
 }
 
 // ---- block scales --------------------------------------------------------------------------------
@@ -140,10 +227,10 @@ __device__ __forceinline__ float pow2_scale_value(uint32_t c) {
 
 // Two values to two codes, to nearest even, a in the low byte; NaN becomes 0x7F.
 template <int FMT>
-__device__ __forceinline__ uint32_t pack_fp8x2(float a, float b) {
+__device__ __forceinline__ uint32_t pack_fp8x2(float2 v) {
     uint16_t r;
-    if constexpr (FMT == kE4M3) asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
-    else asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
+    if constexpr (FMT == kE4M3) asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(v.y), "f"(v.x));
+    else asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(v.y), "f"(v.x));
     return r;
 }
 
@@ -156,44 +243,85 @@ __device__ __forceinline__ float2 unpack_fp8x2(uint32_t two) {
     return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
-// Quantizes the vectors of the `lanes` neighbouring threads that hold a block.  All 32 lanes of the warp call it together.
-template <int FMT>
-__device__ __forceinline__ uint2 quantize_block8(const float (&v)[kVec], int lanes, uint32_t& byte) {
-    uint32_t m = 0;
+// Bits of the largest magnitude; a NaN wins over everything.
+template <int V>
+__device__ __forceinline__ uint32_t amax_bits(const float (&v)[V]) {
+    float m = 0.0f;
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) m = max(m, __float_as_uint(v[j]) & 0x7FFFFFFFu);
-    for (int o = 1; o < lanes; o <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-    byte = pow2_scale_byte<FMT>(m);
-    const float inv = pow2_scale_inverse(byte);
-    return make_uint2(pack_fp8x2<FMT>(v[0] * inv, v[1] * inv) | pack_fp8x2<FMT>(v[2] * inv, v[3] * inv) << 16,
-                      pack_fp8x2<FMT>(v[4] * inv, v[5] * inv) | pack_fp8x2<FMT>(v[6] * inv, v[7] * inv) << 16);
+    for (int j = 0; j < V; j += 2) asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(m), "f"(v[j]), "f"(v[j + 1]));
+    return __float_as_uint(m) & 0x7FFFFFFFu;
 }
 
-template <int FMT>
-__device__ __forceinline__ void dequantize8(uint2 c, float scale, float (&v)[kVec]) {
-    const uint32_t w[2] = {c.x, c.y};
+// Quantizes a vector together with those of the `lanes` neighbouring threads that hold its block.  All 32 lanes of the warp call it.
+template <int FMT, int V>
+__device__ __forceinline__ uint32_t quantize_block(const float (&v)[V], int lanes, uint32_t (&codes)[V / 4]) {
+    uint32_t m = amax_bits<V>(v);
+    for (int o = 1; o < lanes; o <<= 1) m = max(m, __shfl_xor_sync(kFull, m, o));
+    const uint32_t byte = pow2_scale_byte<FMT>(m);
+    const float inv = pow2_scale_inverse(byte);
 #pragma unroll
-    for (int j = 0; j < kVec; j += 2) {
-        const float2 f = unpack_fp8x2<FMT>(w[j >> 2] >> (8 * (j & 3)));
-        v[j] = f.x * scale;
-        v[j + 1] = f.y * scale;
+    for (int j = 0; j < V; j += 4)
+        codes[j / 4] = pack_fp8x2<FMT>(mul2(make_float2(v[j], v[j + 1]), make_float2(inv, inv))) |
+                       pack_fp8x2<FMT>(mul2(make_float2(v[j + 2], v[j + 3]), make_float2(inv, inv))) << 16;
+    return byte;
+}
+
+template <int FMT, int V>
+__device__ __forceinline__ void dequantize_block(const uint32_t* codes, uint32_t byte, float (&v)[V]) {
+    const float s = pow2_scale_value(byte);
+#pragma unroll
+    for (int j = 0; j < V; j += 2) {
+        const float2 f = mul2(unpack_fp8x2<FMT>(codes[j / 4] >> (8 * (j & 2))), make_float2(s, s));
+        v[j] = f.x;
+        v[j + 1] = f.y;
     }
 }
 
-// Quantizes and stores this thread's vector, `vec` in its row; the first lane of a block stores the scale.  The whole warp calls it.
-template <int FMT, bool VEC>
-__device__ __forceinline__ void put_held8(Held8 out, const float (&v)[kVec], size_t row, size_t vec, size_t cols, size_t blocks, int lanes, int lanes_log2, int left) {
-    uint32_t byte;
-    const uint2 c = quantize_block8<FMT>(v, lanes, byte);
-    store_codes8<VEC>(out.codes, row * cols + vec * kVec, left, c);
-    if (left > 0 && (vec & (size_t)(lanes - 1)) == 0) out.scales[row * blocks + (vec >> lanes_log2)] = (uint8_t)byte;
+// ---- vectors of rows -----------------------------------------------------------------------------
+// One vector: its place in the row and what of the row is left there.
+struct Place {
+    size_t row, vec;
+    long long left;   // elements from its first one to the end of the row; <= 0: it lies behind the end
+};
+
+// A wide tensor's vector as fp32.
+template <int DT, bool VEC, int V>
+__device__ __forceinline__ void load_wide(const void* base, size_t at, long long left, float (&v)[V]) {
+    constexpr int EB = elem_bytes(DT);
+    uint32_t w[V * EB / 4];
+    load_bytes<V * EB, VEC>(static_cast<const char*>(base) + at * EB, left >= V ? V * EB : (int)left * EB, w);
+    unpack<DT, V>(w, v);
+}
+template <int DT, bool VEC, int V>
+__device__ __forceinline__ void store_wide(void* base, size_t at, const Place& t, const float (&v)[V]) {
+    constexpr int EB = elem_bytes(DT);
+    uint32_t w[V * EB / 4];
+    pack<DT, V>(v, w);
+    store_bytes<V * EB, EB, VEC>(static_cast<char*>(base) + at * EB, t.left >= V ? V * EB : (int)t.left * EB, t.vec == 0, (t.left - V) * EB, w);
 }
 
-template <int FMT, bool VEC>
-__device__ __forceinline__ void get_held8(Held8 in, float (&v)[kVec], size_t row, size_t vec, size_t cols, size_t blocks, int lanes_log2, int left) {
-    const uint2 c = load_codes8<VEC>(in.codes, row * cols + vec * kVec, left);
-    const float s = left > 0 ? pow2_scale_value(in.scales[row * blocks + (vec >> lanes_log2)]) : 0.0f;
-    dequantize8<FMT>(c, s, v);
+// Quantizes and stores this thread's vector; the first lane of a block stores the scale.  The whole warp calls it.
+template <int FMT, bool VEC, int V>
+__device__ __forceinline__ void put_held(const Held8& out, const float (&v)[V], const Place& t, size_t cols, size_t blocks, int lanes_log2) {
+    uint32_t c[V / 4];
+    const uint32_t byte = quantize_block<FMT, V>(v, 1 << lanes_log2, c);
+    store_bytes<V, 1, VEC>(out.codes + t.row * cols + t.vec * V, t.left >= V ? V : (int)t.left, t.vec == 0, t.left - V, c);
+    if (t.left > 0 && (t.vec & (size_t)((1 << lanes_log2) - 1)) == 0) out.scales[t.row * blocks + (t.vec >> lanes_log2)] = (uint8_t)byte;
+}
+
+template <int FMT, bool VEC, int V>
+__device__ __forceinline__ void get_held(const Held8& in, float (&v)[V], const Place& t, size_t cols, size_t blocks, int lanes_log2) {
+    uint32_t c[V / 4];
+    load_bytes<V, VEC>(in.codes + t.row * cols + t.vec * V, t.left >= V ? V : (int)t.left, c);
+    const uint32_t byte = t.left > 0 ? in.scales[t.row * blocks + (t.vec >> lanes_log2)] : 0u;
+    dequantize_block<FMT, V>(c, byte, v);
+}
+
+// log2 of the lanes that hold a block.
+inline int lanes_log2_of(int block_size, int dtype) {
+    int l = 0;
+    while ((vec_elems(dtype) << l) < block_size) ++l;
+    return l;
 }
 
 }  // namespace mxq

@@ -136,9 +136,10 @@ struct Wide8 {
     void* p;
     size_t stride;
 };
-// Whether its rows can be read and written 16 bytes at a time, in whole vectors of 8 elements.
+// Whether its rows can be read and written in whole vectors of 32 bytes.
 inline bool wide_vec(const Wide8& w, size_t cols, int dtype) {
-    return (reinterpret_cast<uintptr_t>(w.p) & 15u) == 0 && cols % 8 == 0 && w.stride % (dtype == 0 ? 4 : 8) == 0;
+    const size_t v = dtype == 0 ? 8 : 16;
+    return (reinterpret_cast<uintptr_t>(w.p) & 31u) == 0 && cols % v == 0 && w.stride % v == 0;
 }
 constexpr size_t kAct8MaxRows = 0x7FFFFFFF;          // a grid's limit
 constexpr size_t kAct8MaxElems = (size_t)1 << 41;    // rows padded to 128 elements
