@@ -3,18 +3,13 @@
 
 namespace mxq {
 
-// Where a thread's vectors lie.  Vectors are numbered row by row, each row padded to whole blocks; a CTA takes U * 256 consecutive
-// ones, a thread every 256th of them.
+// Vectors are numbered row by row, each row padded to whole blocks; a thread takes one.  Two or four of them a thread, with all loads first,
+// cost resident threads and were slower: store 8192 x 4096 16.2 us with one, 17.1 with two, 16.8 with four, load 8192 x 14336 53.1, 66.2, 71.9.
 struct Rows8 {
     size_t rows, cols, blocks;   // blocks: per row
     size_t vectors;              // per row, padded to whole blocks
-    size_t step_rows, step_vecs; // 256 vectors further on
     int lanes_log2;
 
-    template <int V>
-    __device__ __forceinline__ void measure(Place& t) const {
-        t.left = t.row < rows ? (long long)cols - (long long)(t.vec * V) : 0;
-    }
     template <int V>
     __device__ __forceinline__ Place at(size_t slot) const {
         Place t;
@@ -26,18 +21,7 @@ struct Rows8 {
         } else {
             t.row = slot / vectors, t.vec = slot % vectors;
         }
-        measure<V>(t);
-        return t;
-    }
-    template <int V>
-    __device__ __forceinline__ Place next(Place t) const {
-        t.row += step_rows;
-        t.vec += step_vecs;
-        if (t.vec >= vectors && rows != 1) {
-            t.vec -= vectors;
-            ++t.row;
-        }
-        measure<V>(t);
+        t.left = t.row < rows ? (long long)cols - (long long)(t.vec * V) : 0;
         return t;
     }
 };
@@ -52,58 +36,55 @@ static Rows8 rows8(size_t rows, size_t cols, int B, int dtype, bool flat) {
     r.blocks = (cols + B - 1) / B;
     r.lanes_log2 = lanes_log2_of(B, dtype);
     r.vectors = r.blocks << r.lanes_log2;
-    r.step_rows = rows == 1 ? 0 : kThreads / r.vectors;
-    r.step_vecs = rows == 1 ? kThreads : kThreads % r.vectors;
     return r;
 }
 
-template <int U>
-static unsigned grid_of(const Rows8& r) {
-    const size_t per_cta = (size_t)U * kThreads;
-    return (unsigned)((r.rows * r.vectors + per_cta - 1) / per_cta);
-}
+static unsigned grid_of(const Rows8& r) { return (unsigned)((r.rows * r.vectors + kThreads - 1) / kThreads); }
 
-template <int DT, int FMT, bool VEC, int U>
+template <int DT, int FMT, bool VEC>
 __global__ void __launch_bounds__(kThreads) k_quantize8(const void* x, size_t stride, Rows8 r, Held8 out) {
     constexpr int V = vec_elems(DT);
     wait_for_prior_grid();
     release_dependents();
-    float v[U][V];
-    Place at[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        at[u] = u ? r.next<V>(at[u ? u - 1 : 0]) : r.at<V>((size_t)blockIdx.x * (U * kThreads) + threadIdx.x);
-        load_wide<DT, VEC>(x, at[u].row * stride + at[u].vec * V, at[u].left, v[u]);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) put_held<FMT, VEC>(out, v[u], at[u], r.cols, r.blocks, r.lanes_log2);
+    const Place t = r.at<V>((size_t)blockIdx.x * kThreads + threadIdx.x);
+    float v[V];
+    load_wide<DT, VEC>(x, t.row * stride + t.vec * V, t.left, v);
+    put_held<FMT, VEC>(out, v, t, r.cols, r.blocks, r.lanes_log2);
 }
 
-template <int DT, int FMT, bool VEC, int U>
+template <int DT, int FMT, bool VEC>
 __global__ void __launch_bounds__(kThreads) k_dequantize8(Held8 in, Rows8 r, void* out, size_t stride) {
     constexpr int V = vec_elems(DT);
     wait_for_prior_grid();
     release_dependents();
-    float v[U][V];
-    Place at[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        at[u] = u ? r.next<V>(at[u ? u - 1 : 0]) : r.at<V>((size_t)blockIdx.x * (U * kThreads) + threadIdx.x);
-        get_held<FMT, VEC>(in, v[u], at[u], r.cols, r.blocks, r.lanes_log2);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) store_wide<DT, VEC>(out, at[u].row * stride + at[u].vec * V, at[u], v[u]);
+    const Place t = r.at<V>((size_t)blockIdx.x * kThreads + threadIdx.x);
+    float v[V];
+    get_held<FMT, VEC>(in, v, t, r.cols, r.blocks, r.lanes_log2);
+    store_wide<DT, VEC>(out, t.row * stride + t.vec * V, t, v);
 }
 
-// 1 / (1 + exp(-g)).  The reciprocal's argument is 1 at least; where exp(-g) passes 2^126 (g < -87.3) the sigmoid is taken as zero.
-__device__ __forceinline__ float sigmoid(float g) {
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + expf(-g)));
+// 1 / (1 + exp(-g)) of two values.  The reciprocal's argument is 1 at least; where exp(-g) passes 2^126 (g < -87.3) the sigmoid is taken
+// as zero.  In fp32 exp() is expf().  bf16 tensors, whose results are rounded to 8 significant bits at most, take 2^(-g log2 e) with the
+// exponent rounded to binary32: off by (1.3 |g| + 4) 2^-24 relative where g is negative and by less where it is positive, 1e-6 at
+// g = -16; a third fewer instructions in kernels that the issue slots bound.
+template <int DT>
+__device__ __forceinline__ float2 sigmoid2(float2 g) {
+    float2 e, r;
+    if constexpr (DT == kBF16) {
+        const float2 t = mul2(g, make_float2(-1.4426950408889634f, -1.4426950408889634f));
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(t.x));
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(t.y));
+    } else {
+        e = make_float2(expf(-g.x), expf(-g.y));
+    }
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(1.0f + e.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(1.0f + e.y));
     return r;
 }
 
+// Registers for five (six) CTAs an SM: 8192 x 14336 with the checkpoints 129 us (four 132, six 140), without 93 with five or six (four 100).
 template <int DT, int FMT, bool VEC, bool KEEP>
-__global__ void __launch_bounds__(kThreads) k_swiglu8(const void* gate, size_t gate_stride, const void* up, size_t up_stride, Rows8 r, Held8 out, Held8 out_gate, Held8 out_up) {
+__global__ void __launch_bounds__(kThreads, VEC ? (KEEP ? 5 : 6) : 1) k_swiglu8(const void* gate, size_t gate_stride, const void* up, size_t up_stride, Rows8 r, Held8 out, Held8 out_gate, Held8 out_up) {
     constexpr int V = vec_elems(DT);
     wait_for_prior_grid();
     release_dependents();
@@ -117,14 +98,16 @@ __global__ void __launch_bounds__(kThreads) k_swiglu8(const void* gate, size_t g
     }
 #pragma unroll
     for (int j = 0; j < V; j += 2) {
-        const float2 a = mul2(mul2(make_float2(g[j], g[j + 1]), make_float2(sigmoid(g[j]), sigmoid(g[j + 1]))), make_float2(p[j], p[j + 1]));
+        const float2 gg = make_float2(g[j], g[j + 1]);
+        const float2 a = mul2(mul2(gg, sigmoid2<DT>(gg)), make_float2(p[j], p[j + 1]));
         g[j] = a.x, g[j + 1] = a.y;
     }
     put_held<FMT, VEC>(out, g, t, r.cols, r.blocks, r.lanes_log2);
 }
 
+// Six CTAs an SM: 8192 x 14336 150 us (five 154, four 175).
 template <int DT, int FMT, bool VEC>
-__global__ void __launch_bounds__(kThreads) k_swiglu8_backward(const void* dy, size_t dy_stride, Held8 gate, Held8 up, Rows8 r, void* dgate, size_t dgate_stride, void* dup, size_t dup_stride) {
+__global__ void __launch_bounds__(kThreads, VEC ? 6 : 1) k_swiglu8_backward(const void* dy, size_t dy_stride, Held8 gate, Held8 up, Rows8 r, void* dgate, size_t dgate_stride, void* dup, size_t dup_stride) {
     constexpr int V = vec_elems(DT);
     wait_for_prior_grid();
     release_dependents();
@@ -135,7 +118,7 @@ __global__ void __launch_bounds__(kThreads) k_swiglu8_backward(const void* dy, s
     get_held<FMT, VEC>(up, p, t, r.cols, r.blocks, r.lanes_log2);
 #pragma unroll
     for (int j = 0; j < V; j += 2) {
-        const float2 gg = make_float2(g[j], g[j + 1]), s = make_float2(sigmoid(g[j]), sigmoid(g[j + 1]));
+        const float2 gg = make_float2(g[j], g[j + 1]), s = sigmoid2<DT>(gg);
         const float2 ds = mul2(make_float2(d[j], d[j + 1]), s);
         const float2 du = mul2(ds, gg);
         const float2 slope = fma2(gg, make_float2(1.0f - s.x, 1.0f - s.y), make_float2(1.0f, 1.0f));
@@ -156,20 +139,18 @@ static cudaError_t pick(int dtype, int fmt, bool vec, F f) {
 }
 
 cudaError_t launch_quantize8(const Wide8& x, size_t rows, size_t cols, int B, int dtype, int fmt, const Held8& out, cudaStream_t s) {
-    constexpr int U = 2;
     const Rows8 r = rows8(rows, cols, B, dtype, x.stride == cols && cols % B == 0);
     return pick(dtype, fmt, wide_vec(x, cols, dtype), [&](auto dt, auto fm, auto vec) {
         count_launch();
-        return launch_pdl(k_quantize8<dt(), fm(), vec(), U>, grid_of<U>(r), kThreads, 0, s, (const void*)x.p, x.stride, r, out);
+        return launch_pdl(k_quantize8<dt(), fm(), vec()>, grid_of(r), kThreads, 0, s, (const void*)x.p, x.stride, r, out);
     });
 }
 
 cudaError_t launch_dequantize8(const Held8& in, size_t rows, size_t cols, int B, int dtype, int fmt, const Wide8& out, cudaStream_t s) {
-    constexpr int U = 2;
     const Rows8 r = rows8(rows, cols, B, dtype, out.stride == cols && cols % B == 0);
     return pick(dtype, fmt, wide_vec(out, cols, dtype), [&](auto dt, auto fm, auto vec) {
         count_launch();
-        return launch_pdl(k_dequantize8<dt(), fm(), vec(), U>, grid_of<U>(r), kThreads, 0, s, in, r, out.p, out.stride);
+        return launch_pdl(k_dequantize8<dt(), fm(), vec()>, grid_of(r), kThreads, 0, s, in, r, out.p, out.stride);
     });
 }
 
@@ -179,7 +160,7 @@ cudaError_t launch_swiglu8(const Wide8& gate, const Wide8& up, size_t rows, size
     return pick(dtype, fmt, wide_vec(gate, cols, dtype) && wide_vec(up, cols, dtype), [&](auto dt, auto fm, auto vec) {
         count_launch();
         auto kernel = out_gate.codes ? k_swiglu8<dt(), fm(), vec(), true> : k_swiglu8<dt(), fm(), vec(), false>;
-        return launch_pdl(kernel, grid_of<1>(r), kThreads, 0, s, (const void*)gate.p, gate.stride, (const void*)up.p, up.stride, r, out, out_gate, out_up);
+        return launch_pdl(kernel, grid_of(r), kThreads, 0, s, (const void*)gate.p, gate.stride, (const void*)up.p, up.stride, r, out, out_gate, out_up);
     });
 }
 
@@ -188,7 +169,7 @@ cudaError_t launch_swiglu8_backward(const Wide8& dy, const Held8& gate, const He
     const Rows8 r = rows8(rows, cols, B, dtype, dy.stride == cols && dgate.stride == cols && dup.stride == cols && cols % B == 0);
     return pick(dtype, fmt, wide_vec(dy, cols, dtype) && wide_vec(dgate, cols, dtype) && wide_vec(dup, cols, dtype), [&](auto dt, auto fm, auto vec) {
         count_launch();
-        return launch_pdl(k_swiglu8_backward<dt(), fm(), vec()>, grid_of<1>(r), kThreads, 0, s, (const void*)dy.p, dy.stride, gate, up, r, dgate.p, dgate.stride, dup.p,
+        return launch_pdl(k_swiglu8_backward<dt(), fm(), vec()>, grid_of(r), kThreads, 0, s, (const void*)dy.p, dy.stride, gate, up, r, dgate.p, dgate.stride, dup.p,
                           dup.stride);
     });
 }

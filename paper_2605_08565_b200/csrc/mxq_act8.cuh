@@ -206,6 +206,23 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
     return r;
 }
 
+// ---- asynchronous copies into shared memory: a thread reads back only what it copied itself ----
+__device__ __forceinline__ void copy_async16(void* to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_async8(void* to, const void* from) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_async4(void* to, const void* from) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// Waits until at most `N` of this thread's groups are under way.
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
 // ---- block scales --------------------------------------------------------------------------------
 // Scale byte of a block whose largest magnitude has these bits: c = e + 127 with the smallest e >= -127 for which
 // amax <= top * 2^e, top = 1.75 * 2^t the largest element (t = 8 for E4M3, 15 for E5M2).  amax = m * 2^E with 1 <= m < 2 gives
@@ -225,22 +242,29 @@ __device__ __forceinline__ float pow2_scale_value(uint32_t c) {
     return __uint_as_float(c == 0xFFu ? 0x7FC00000u : c == 0u ? 0x00400000u : c << 23);
 }
 
-// Two values to two codes, to nearest even, a in the low byte; NaN becomes 0x7F.
+// Four values to four codes, to nearest even, the first in the low byte; NaN becomes 0x7F.
 template <int FMT>
-__device__ __forceinline__ uint32_t pack_fp8x2(float2 v) {
-    uint16_t r;
-    if constexpr (FMT == kE4M3) asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(v.y), "f"(v.x));
-    else asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(v.y), "f"(v.x));
+__device__ __forceinline__ uint32_t pack_fp8x4(float2 a, float2 b) {
+    uint32_t r;
+    if constexpr (FMT == kE4M3)
+        asm("{\n .reg .b16 l, h;\n cvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n cvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n mov.b32 %0, {l, h};\n}"
+            : "=r"(r) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    else
+        asm("{\n .reg .b16 l, h;\n cvt.rn.satfinite.e5m2x2.f32 l, %2, %1;\n cvt.rn.satfinite.e5m2x2.f32 h, %4, %3;\n mov.b32 %0, {l, h};\n}"
+            : "=r"(r) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return r;
 }
 
-// Every 8-bit code is a binary16 value.
+// Four codes to four values; every 8-bit code is a binary16 value.
 template <int FMT>
-__device__ __forceinline__ float2 unpack_fp8x2(uint32_t two) {
-    uint32_t h;
-    if constexpr (FMT == kE4M3) asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
-    else asm("cvt.rn.f16x2.e5m2x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
-    return __half22float2(*reinterpret_cast<const __half2*>(&h));
+__device__ __forceinline__ void unpack_fp8x4(uint32_t four, float2& a, float2& b) {
+    uint32_t l, h;
+    if constexpr (FMT == kE4M3)
+        asm("{\n .reg .b16 x, y;\n mov.b32 {x, y}, %2;\n cvt.rn.f16x2.e4m3x2 %0, x;\n cvt.rn.f16x2.e4m3x2 %1, y;\n}" : "=r"(l), "=r"(h) : "r"(four));
+    else
+        asm("{\n .reg .b16 x, y;\n mov.b32 {x, y}, %2;\n cvt.rn.f16x2.e5m2x2 %0, x;\n cvt.rn.f16x2.e5m2x2 %1, y;\n}" : "=r"(l), "=r"(h) : "r"(four));
+    a = __half22float2(*reinterpret_cast<const __half2*>(&l));
+    b = __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
 // Bits of the largest magnitude; a NaN wins over everything.
@@ -252,17 +276,18 @@ __device__ __forceinline__ uint32_t amax_bits(const float (&v)[V]) {
     return __float_as_uint(m) & 0x7FFFFFFFu;
 }
 
-// Quantizes a vector together with those of the `lanes` neighbouring threads that hold its block.  All 32 lanes of the warp call it.
+// Quantizes a vector together with those of the 2^lanes_log2 neighbouring threads that hold its block.  All 32 lanes of the warp call it.
 template <int FMT, int V>
-__device__ __forceinline__ uint32_t quantize_block(const float (&v)[V], int lanes, uint32_t (&codes)[V / 4]) {
+__device__ __forceinline__ uint32_t quantize_block(const float (&v)[V], int lanes_log2, uint32_t (&codes)[V / 4]) {
     uint32_t m = amax_bits<V>(v);
-    for (int o = 1; o < lanes; o <<= 1) m = max(m, __shfl_xor_sync(kFull, m, o));
+#pragma unroll
+    for (int l = 0; l < (V == 16 ? 3 : 4); ++l)
+        if (l < lanes_log2) m = max(m, __shfl_xor_sync(kFull, m, 1 << l));
     const uint32_t byte = pow2_scale_byte<FMT>(m);
     const float inv = pow2_scale_inverse(byte);
 #pragma unroll
     for (int j = 0; j < V; j += 4)
-        codes[j / 4] = pack_fp8x2<FMT>(mul2(make_float2(v[j], v[j + 1]), make_float2(inv, inv))) |
-                       pack_fp8x2<FMT>(mul2(make_float2(v[j + 2], v[j + 3]), make_float2(inv, inv))) << 16;
+        codes[j / 4] = pack_fp8x4<FMT>(mul2(make_float2(v[j], v[j + 1]), make_float2(inv, inv)), mul2(make_float2(v[j + 2], v[j + 3]), make_float2(inv, inv)));
     return byte;
 }
 
@@ -270,10 +295,11 @@ template <int FMT, int V>
 __device__ __forceinline__ void dequantize_block(const uint32_t* codes, uint32_t byte, float (&v)[V]) {
     const float s = pow2_scale_value(byte);
 #pragma unroll
-    for (int j = 0; j < V; j += 2) {
-        const float2 f = mul2(unpack_fp8x2<FMT>(codes[j / 4] >> (8 * (j & 2))), make_float2(s, s));
-        v[j] = f.x;
-        v[j + 1] = f.y;
+    for (int j = 0; j < V; j += 4) {
+        float2 a, b;
+        unpack_fp8x4<FMT>(codes[j / 4], a, b);
+        a = mul2(a, make_float2(s, s)), b = mul2(b, make_float2(s, s));
+        v[j] = a.x, v[j + 1] = a.y, v[j + 2] = b.x, v[j + 3] = b.y;
     }
 }
 
@@ -304,7 +330,7 @@ __device__ __forceinline__ void store_wide(void* base, size_t at, const Place& t
 template <int FMT, bool VEC, int V>
 __device__ __forceinline__ void put_held(const Held8& out, const float (&v)[V], const Place& t, size_t cols, size_t blocks, int lanes_log2) {
     uint32_t c[V / 4];
-    const uint32_t byte = quantize_block<FMT, V>(v, 1 << lanes_log2, c);
+    const uint32_t byte = quantize_block<FMT, V>(v, lanes_log2, c);
     store_bytes<V, 1, VEC>(out.codes + t.row * cols + t.vec * V, t.left >= V ? V : (int)t.left, t.vec == 0, t.left - V, c);
     if (t.left > 0 && (t.vec & (size_t)((1 << lanes_log2) - 1)) == 0) out.scales[t.row * blocks + (t.vec >> lanes_log2)] = (uint8_t)byte;
 }
@@ -315,6 +341,12 @@ __device__ __forceinline__ void get_held(const Held8& in, float (&v)[V], const P
     load_bytes<V, VEC>(in.codes + t.row * cols + t.vec * V, t.left >= V ? V : (int)t.left, c);
     const uint32_t byte = t.left > 0 ? in.scales[t.row * blocks + (t.vec >> lanes_log2)] : 0u;
     dequantize_block<FMT, V>(c, byte, v);
+}
+
+template <int V>
+__device__ __forceinline__ void store_codes(uint8_t* to, const uint32_t (&c)[V / 4]) {
+    if constexpr (V == 16) *reinterpret_cast<uint4*>(to) = make_uint4(c[0], c[1], c[2], c[3]);
+    else *reinterpret_cast<uint2*>(to) = make_uint2(c[0], c[1]);
 }
 
 // log2 of the lanes that hold a block.

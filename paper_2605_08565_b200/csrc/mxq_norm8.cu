@@ -1,6 +1,9 @@
 // Root-mean-square norm of rows with the residual's addition and an output in block-scaled 8 bits, and its gradient from the 8-bit
 // checkpoint of the sum.
+#include <atomic>
+
 #include "mxq_act8.cuh"
+
 
 namespace mxq {
 
@@ -18,18 +21,19 @@ template <bool SMALL>
 __device__ __forceinline__ float row_sum(float v, int group, float* scratch) {
     if constexpr (SMALL) {
         for (int o = group >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
-        return v;
-    }
+    } else {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
-    const int warps = blockDim.x >> 5;
-    if (warps == 1) return v;
-    const int top = 32 - __clz(warps - 1);   // log2 of the warps, rounded up
-    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
-    __syncthreads();
-    const int i = threadIdx.x & ((1 << top) - 1);
-    v = i < warps ? scratch[i] : 0.0f;
-    for (int o = 1 << (top - 1); o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
+        const int warps = blockDim.x >> 5;
+        if (warps > 1) {
+            const int top = 32 - __clz(warps - 1);   // log2 of the warps, rounded up
+            if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
+            __syncthreads();
+            const int i = threadIdx.x & ((1 << top) - 1);
+            v = i < warps ? scratch[i] : 0.0f;
+            for (int o = 1 << (top - 1); o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
+        }
+    }
     return v;
 }
 
@@ -48,9 +52,9 @@ __device__ __forceinline__ void load_weight(const void* weight, int weight_dtype
     else load_wide<kF32, VEC>(weight, t.vec * V, t.left, w);
 }
 
-template <int DT, int FMT, bool VEC, int K, bool SMALL>
-__global__ void __launch_bounds__(SMALL ? 256 : 1024) k_add_rmsnorm8(const void* x, size_t x_stride, const void* residual, size_t r_stride, const void* weight, int weight_dtype,
-                                                                     float eps, NormShape n, void* out_sum, size_t s_stride, Held8 out, Held8 kept, float* out_rstd) {
+template <int DT, int FMT, bool VEC, int K, bool SMALL, int T>
+__global__ void __launch_bounds__(T) k_add_rmsnorm8(const void* x, size_t x_stride, const void* residual, size_t r_stride, const void* weight, int weight_dtype,
+                                                                     float eps, float inv_cols, NormShape n, void* out_sum, size_t s_stride, Held8 out, Held8 kept, float* out_rstd) {
     constexpr int V = vec_elems(DT);
     __shared__ float scratch[32];
     wait_for_prior_grid();
@@ -77,7 +81,7 @@ __global__ void __launch_bounds__(SMALL ? 256 : 1024) k_add_rmsnorm8(const void*
         if (kept.codes) put_held<FMT, VEC>(kept, h[k], t, n.cols, n.blocks, n.lanes_log2);
     }
     sq = row_sum<SMALL>(sq, n.group, scratch);
-    const float rstd = 1.0f / sqrtf(sq / (float)n.cols + eps);
+    const float rstd = rsqrtf(__fmaf_rn(sq, inv_cols, eps));
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const Place t = place_of<V, SMALL>(n, row, k);
@@ -95,9 +99,9 @@ __global__ void __launch_bounds__(SMALL ? 256 : 1024) k_add_rmsnorm8(const void*
 
 // A CTA takes every gridDim.x-th row (or group of rows); a thread holds the same K vectors of each and adds up its columns' part of the
 // weight's gradient.
-template <int DT, int FMT, bool VEC, int K, bool SMALL>
-__global__ void __launch_bounds__(SMALL ? 256 : 1024) k_add_rmsnorm8_backward(const void* dy, size_t dy_stride, const void* dsum, size_t ds_stride, const void* weight,
-                                                                              int weight_dtype, Held8 kept, const float* rstd, NormShape n, void* dx, size_t dx_stride,
+template <int DT, int FMT, bool VEC, int K, bool SMALL, int T>
+__global__ void __launch_bounds__(T) k_add_rmsnorm8_backward(const void* dy, size_t dy_stride, const void* dsum, size_t ds_stride, const void* weight,
+                                                                              int weight_dtype, Held8 kept, const float* rstd, float inv_cols, NormShape n, void* dx, size_t dx_stride,
                                                                               float* parts) {
     constexpr int V = vec_elems(DT);
     __shared__ float scratch[2][32];
@@ -131,7 +135,7 @@ __global__ void __launch_bounds__(SMALL ? 256 : 1024) k_add_rmsnorm8_backward(co
                 dot = __fmaf_rn(wd[k][j], xh[k][j], dot);
             }
         }
-        const float c = row_sum<SMALL>(dot, n.group, scratch[turn]) / (float)n.cols;
+        const float c = row_sum<SMALL>(dot, n.group, scratch[turn]) * inv_cols;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const Place t = place_of<V, SMALL>(n, row, k);
@@ -166,23 +170,268 @@ __global__ void __launch_bounds__(SMALL ? 256 : 1024) k_add_rmsnorm8_backward(co
     }
 }
 
-// dweight[c] = sum over the parts, in a fixed order: each of 8 warps every eighth part, then the warps' sums in order.
-__global__ void __launch_bounds__(256) k_rmsnorm8_dweight(const float* parts, int n_parts, size_t cols, float* dweight) {
-    __shared__ float sums[8][32];
+// ---- rows of whole vectors, one vector a thread ------------------------------------------------------------------------------------
+// A CTA takes every gridDim.x-th row and copies the next one into shared memory while it works on the present one, so that what is under way
+// from memory does not depend on the threads' registers, nor stop while the CTA meets in its barrier.  T: the most threads of a CTA.
+
+// The 32 vectors of a warp: each lane copies two of their 64 pieces of 16 bytes, 512 bytes apart, so that an instruction asks for whole
+// sectors (each lane its own two pieces: twice the requests to L2).  Piece p lies at p ^ (p >> 3 & 1), without which the lanes' reads of every
+// second piece would meet in the banks.
+struct WarpCopy {
+    bool low, high;   // whether the row has this lane's pieces
+    int at;
+    __device__ __forceinline__ explicit WarpCopy(long long bytes) {   // of the row, from the warp's first vector on
+        const int lane = threadIdx.x & 31;
+        low = lane * 16 < bytes;
+        high = lane * 16 + 512 < bytes;
+        at = lane ^ (lane >> 3 & 1);
+    }
+    __device__ __forceinline__ void operator()(uint4* to, const char* piece) const {
+        if (low) copy_async16(to + at, piece);
+        if (high) copy_async16(to + at + 32, piece + 512);
+    }
+};
+__device__ __forceinline__ void read32(const uint4* from, uint32_t (&w)[8]) {
+    const int p = 2 * (threadIdx.x & 31), flip = p >> 3 & 1;
+    const uint4 a = from[p ^ flip], b = from[(p + 1) ^ flip];
+    w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+}
+
+// Sum over the CTA, the same bits in every thread.  sums: T / 32 floats, those of warps that the CTA does not have zeros, which nothing else
+// uses between the barrier inside and the next one.
+template <int T>
+__device__ __forceinline__ float cta_sum(float v, float* sums) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
+    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = v;
+    __syncthreads();
+    float4 t = reinterpret_cast<const float4*>(sums)[0];
+#pragma unroll
+    for (int i = 1; i < (T + 127) / 128; ++i) {
+        const float4 u = reinterpret_cast<const float4*>(sums)[i];
+        t.x += u.x, t.y += u.y, t.z += u.z, t.w += u.w;
+    }
+    return (t.x + t.y) + (t.z + t.w);
+}
+
+// Two CTAs of 256 threads an SM and the registers that they leave are faster than three with fewer (8192 x 4096, us: with the residual and
+// the checkpoint 43.5 / 49.1, with the residual 37.7 / 39.9) and slower without a residual (with the checkpoint 27.9 / 24.7).  CTAs of 320 and
+// 384 threads would else be alone on their SM.
+template <int DT, int FMT, bool RES, bool KEEP, int T>
+__global__ void __launch_bounds__(T, T == 256 ? (RES ? 2 : 3) : T <= 384 ? 2 : 1)
+    k_add_rmsnorm8_rows(const char* x, size_t x_step, const char* residual, size_t r_step, const void* weight, int weight_dtype, float eps, float inv_cols, NormShape n,
+                        char* out_sum, size_t s_step, Held8 out, Held8 kept, float* out_rstd) {
+    constexpr int V = vec_elems(DT);
+    const int n_thr = blockDim.x, slot_size = (RES ? 4 : 2) * n_thr;
+    extern __shared__ uint4 ring[];
+    __shared__ float4 sums[2][(T + 127) / 128];
+    wait_for_prior_grid();
+    release_dependents();
+    const Place t = place_of<V, false>(n, 0, 0);
+    const bool here = t.left > 0, leads = here && (threadIdx.x & ((1u << n.lanes_log2) - 1)) == 0;
+    const int warp0 = threadIdx.x & ~31;   // the warp's first vector
+    const WarpCopy copy(((long long)n.cols - (long long)warp0 * V) * (32 / V));
+    const size_t step = gridDim.x;
+    size_t row = blockIdx.x;
+    const char* px = x + row * x_step + warp0 * 32 + (threadIdx.x & 31) * 16;
+    const char* pr = residual + row * r_step + warp0 * 32 + (threadIdx.x & 31) * 16;
+    char* ps = out_sum + row * s_step + threadIdx.x * 32;
+    size_t code = row * n.cols + threadIdx.x * V, scale = row * n.blocks + (threadIdx.x >> n.lanes_log2);
+    uint4* slot = ring + warp0 * 2;
+    uint4* other = slot + slot_size;
+    if (threadIdx.x < sizeof(sums) / 4) reinterpret_cast<float*>(sums)[threadIdx.x] = 0.0f;
+    copy(slot, px);
+    if constexpr (RES) copy(slot + 2 * n_thr, pr);
+    copy_commit();
+    float w[V];
+    load_weight<true, V>(weight, weight_dtype, t, w);
+    __syncthreads();   // the zeros in `sums`
+    for (int turn = 0; row < n.rows; row += step, turn ^= 1) {
+        __syncwarp();   // the other lanes have read what the next copies replace
+        px += step * x_step;
+        pr += step * r_step;
+        if (row + step < n.rows) {
+            copy(other, px);
+            if constexpr (RES) copy(other + 2 * n_thr, pr);
+        }
+        copy_commit();
+        copy_wait<1>();
+        __syncwarp();
+        float h[V];
+        uint32_t a[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+        if (here) read32(slot, a);
+        unpack<DT, V>(a, h);
+        if constexpr (RES) {
+            float r[V];
+            if (here) read32(slot + 2 * n_thr, a);
+            unpack<DT, V>(a, r);
+#pragma unroll
+            for (int j = 0; j < V; ++j) h[j] += r[j];
+            pack<DT, V>(h, a);
+            unpack<DT, V>(a, h);
+            if (here) store256(ps, a);
+            ps += step * s_step;
+        }
+        float2 sq = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int j = 0; j < V; j += 2) sq = fma2(make_float2(h[j], h[j + 1]), make_float2(h[j], h[j + 1]), sq);
+        uint32_t c[V / 4];
+        if constexpr (KEEP) {
+            const uint32_t byte = quantize_block<FMT, V>(h, n.lanes_log2, c);
+            if (here) store_codes<V>(kept.codes + code, c);
+            if (leads) kept.scales[scale] = (uint8_t)byte;
+        }
+        const float rstd = rsqrtf(__fmaf_rn(cta_sum<T>(sq.x + sq.y, reinterpret_cast<float*>(sums[turn])), inv_cols, eps));
+        if (out_rstd && threadIdx.x == 0) out_rstd[row] = rstd;
+#pragma unroll
+        for (int j = 0; j < V; j += 2) {
+            const float2 y = mul2(mul2(make_float2(h[j], h[j + 1]), make_float2(rstd, rstd)), make_float2(w[j], w[j + 1]));
+            h[j] = y.x, h[j + 1] = y.y;
+        }
+        const uint32_t byte = quantize_block<FMT, V>(h, n.lanes_log2, c);
+        if (here) store_codes<V>(out.codes + code, c);
+        if (leads) out.scales[scale] = (uint8_t)byte;
+        code += step * n.cols;
+        scale += step * n.blocks;
+        uint4* const done = slot;
+        slot = other;
+        other = done;
+    }
+}
+
+// The scale bytes of a warp's 32 vectors and the row's rstd are copied as well, in the aligned words that hold them (kMeta a warp): a register
+// that is loaded one row ahead has to arrive within that row, because the loop's end moves it (8192 x 4096: 62 us, and 47 like this).
+constexpr int kMeta = 12;   // 32 bytes off the grid lie in 9 words; rstd; 2 unused
+
+// 117 registers: two CTAs of up to 320 threads an SM (8192 x 5120 62.5 us with one, 51.4 with two).  Limited to what a third one, or a second
+// one of 384 threads, leaves, the compiler spills (8192 x 4096 41.9 -> 62.4, 8192 x 6144 68.8 -> 88.8).
+template <int DT, int FMT, bool DSUM, int T>
+__global__ void __launch_bounds__(T, T <= 320 ? 2 : 1)
+    k_add_rmsnorm8_backward_rows(const char* dy, size_t dy_step, const char* dsum, size_t ds_step, const void* weight, int weight_dtype, Held8 kept, const float* rstd,
+                                 float inv_cols, NormShape n, char* dx, size_t dx_step, float* parts) {
+    constexpr int V = vec_elems(DT), C = DSUM ? 5 : 3;
+    const int n_thr = blockDim.x, slot_size = C * n_thr + kMeta * n_thr / 128;
+    extern __shared__ uint4 ring[];
+    __shared__ float4 sums[2][(T + 127) / 128];
+    wait_for_prior_grid();
+    release_dependents();
+    const Place t = place_of<V, false>(n, 0, 0);
+    const bool here = t.left > 0;
+    const int lane = threadIdx.x & 31, warp0 = threadIdx.x & ~31;
+    const WarpCopy copy(((long long)n.cols - (long long)warp0 * V) * (32 / V));
+    const size_t step = gridDim.x;
+    size_t row = blockIdx.x;
+    const char* py = dy + row * dy_step + warp0 * 32 + lane * 16;
+    const char* ps = dsum + row * ds_step + warp0 * 32 + lane * 16;
+    const uint8_t* pc = kept.codes + row * n.cols + threadIdx.x * V;
+    const uint8_t* pb = kept.scales + row * n.blocks + (warp0 >> n.lanes_log2);   // the warp's first scale byte
+    const int bytes = (int)min((long long)(32 >> n.lanes_log2), (long long)n.blocks - (warp0 >> n.lanes_log2));
+    const float* pr = rstd + row;
+    char* px = dx + row * dx_step + threadIdx.x * 32;
+    uint4* slot = ring;
+    uint4* other = ring + slot_size;
+    auto fetch = [&](uint4* to) {
+        copy(to + warp0 * 2, py);
+        if constexpr (DSUM) copy(to + 2 * n_thr + warp0 * 2, ps);
+        if (here) {
+            if constexpr (V == 16) copy_async16(to + (C - 1) * n_thr + threadIdx.x, pc);
+            else copy_async8(to + (C - 1) * n_thr + threadIdx.x, pc);
+        }
+        uint32_t* const meta = reinterpret_cast<uint32_t*>(to + C * n_thr) + kMeta * (threadIdx.x / 32);
+        const int off = (int)(reinterpret_cast<uintptr_t>(pb) & 3u);
+        if (lane < 9 ? bytes > 0 && 4 * lane < off + bytes : lane == 9) copy_async4(meta + lane, lane < 9 ? (const void*)(pb - off + 4 * lane) : (const void*)pr);
+    };
+    if (threadIdx.x < sizeof(sums) / 4) reinterpret_cast<float*>(sums)[threadIdx.x] = 0.0f;
+    fetch(slot);
+    copy_commit();
+    float w[V], dw[V];
+    load_weight<true, V>(weight, weight_dtype, t, w);
+#pragma unroll
+    for (int j = 0; j < V; ++j) dw[j] = 0.0f;
+    __syncthreads();   // the zeros in `sums`
+    for (int turn = 0; row < n.rows; row += step, turn ^= 1) {
+        const unsigned off = (unsigned)(reinterpret_cast<uintptr_t>(pb) & 3u) + (lane >> n.lanes_log2);
+        __syncwarp();   // the other lanes have read what the next copies replace
+        py += step * dy_step, ps += step * ds_step, pc += step * n.cols, pb += step * n.blocks, pr += step;
+        if (row + step < n.rows) fetch(other);
+        copy_commit();
+        copy_wait<1>();
+        __syncwarp();
+        const uint32_t* const meta = reinterpret_cast<const uint32_t*>(slot + C * n_thr) + kMeta * (threadIdx.x / 32);
+        const float rs = __uint_as_float(meta[9]);
+        float wd[V], xh[V];
+        {
+            uint32_t a[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u}, c[V / 4] = {}, byte = 0u;
+            if (here) {
+                read32(slot + warp0 * 2, a);
+                const uint4 q = slot[(C - 1) * n_thr + threadIdx.x];
+                c[0] = q.x, c[1] = q.y;
+                if constexpr (V == 16) c[2] = q.z, c[3] = q.w;
+                byte = reinterpret_cast<const uint8_t*>(meta)[off];
+            }
+            unpack<DT, V>(a, wd);
+            dequantize_block<FMT, V>(c, byte, xh);
+        }
+        float2 dot = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int j = 0; j < V; j += 2) {
+            const float2 d = make_float2(wd[j], wd[j + 1]);
+            const float2 h = mul2(make_float2(xh[j], xh[j + 1]), make_float2(rs, rs));
+            const float2 s = fma2(d, h, make_float2(dw[j], dw[j + 1]));
+            const float2 e = mul2(d, make_float2(w[j], w[j + 1]));
+            dot = fma2(e, h, dot);
+            dw[j] = s.x, dw[j + 1] = s.y, xh[j] = h.x, xh[j + 1] = h.y, wd[j] = e.x, wd[j + 1] = e.y;
+        }
+        const float c = -cta_sum<T>(dot.x + dot.y, reinterpret_cast<float*>(sums[turn])) * inv_cols;
+        float ds[V];
+        uint32_t b[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+        if constexpr (DSUM)
+            if (here) read32(slot + 2 * n_thr + warp0 * 2, b);
+        unpack<DT, V>(b, ds);
+#pragma unroll
+        for (int j = 0; j < V; j += 2) {
+            float2 e = fma2(make_float2(xh[j], xh[j + 1]), make_float2(c, c), make_float2(wd[j], wd[j + 1]));
+            if constexpr (DSUM) e = fma2(e, make_float2(rs, rs), make_float2(ds[j], ds[j + 1]));
+            else e = mul2(e, make_float2(rs, rs));
+            ds[j] = e.x, ds[j + 1] = e.y;
+        }
+        pack<DT, V>(ds, b);
+        if (here) store256(px, b);
+        px += step * dx_step;
+        uint4* const done = slot;
+        slot = other;
+        other = done;
+    }
+    if (!parts || !here) return;
+#pragma unroll
+    for (int j = 0; j < V; j += 8) {
+        uint32_t b[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(dw[j + i]);
+        store256(parts + blockIdx.x * n.cols + t.vec * V + j, b);
+    }
+}
+
+// dweight[c] = sum over the parts, in a fixed order: each of 32 warps every 32nd part, then a tree over the warps.  With 8 warps a warp's
+// loads come in turns, and the launch takes 2 us more.
+__global__ void __launch_bounds__(1024) k_rmsnorm8_dweight(const float* parts, int n_parts, size_t cols, float* dweight) {
+    __shared__ float sums[32][33];
     wait_for_prior_grid();
     release_dependents();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const size_t col = (size_t)blockIdx.x * 32 + lane;
     float s = 0.0f;
-    if (col < cols)
-        for (int p = warp; p < n_parts; p += 8) s += parts[(size_t)p * cols + col];
+    if (col < cols) {
+#pragma unroll 8
+        for (int p = warp; p < n_parts; p += 32) s += parts[(size_t)p * cols + col];
+    }
     sums[warp][lane] = s;
     __syncthreads();
-    if (warp == 0 && col < cols) {
+    s = sums[lane][warp];   // warp: the column, lane: the part
 #pragma unroll
-        for (int w = 1; w < 8; ++w) s += sums[w][lane];
-        dweight[col] = s;
-    }
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
+    const size_t mine = (size_t)blockIdx.x * 32 + warp;
+    if (lane == 0 && mine < cols) dweight[mine] = s;
 }
 
 // Shape, threads of a CTA and vectors of a thread for rows of this kind.
@@ -218,13 +467,46 @@ static cudaError_t pick(int dtype, int fmt, bool vec, const NormLaunch& l, F f) 
     using Yes = integral_constant<bool, true>;
     using No = integral_constant<bool, false>;
     auto by_k = [&](auto dt, auto fm, auto v) {
-        if (l.n.group) return f(dt, fm, v, integral_constant<int, 1>{}, Yes{});
-        return l.K == 1   ? f(dt, fm, v, integral_constant<int, 1>{}, No{})
-               : l.K == 2 ? f(dt, fm, v, integral_constant<int, 2>{}, No{})
-                          : f(dt, fm, v, integral_constant<int, 4>{}, No{});
+        if (l.n.group) return f(dt, fm, v, integral_constant<int, 1>{}, Yes{}, integral_constant<int, 256>{});
+        if (l.K == 1 && l.threads <= 256) return f(dt, fm, v, integral_constant<int, 1>{}, No{}, integral_constant<int, 256>{});
+        if (l.K == 1 && l.threads <= 512) return f(dt, fm, v, integral_constant<int, 1>{}, No{}, integral_constant<int, 512>{});
+        return l.K == 1   ? f(dt, fm, v, integral_constant<int, 1>{}, No{}, integral_constant<int, 1024>{})
+               : l.K == 2 ? f(dt, fm, v, integral_constant<int, 2>{}, No{}, integral_constant<int, 1024>{})
+                          : f(dt, fm, v, integral_constant<int, 4>{}, No{}, integral_constant<int, 1024>{});
     };
     auto by_vec = [&](auto dt, auto fm) { return vec ? by_k(dt, fm, Yes{}) : by_k(dt, fm, No{}); };
     auto by_fmt = [&](auto dt) { return fmt == kE4M3 ? by_vec(dt, integral_constant<int, kE4M3>{}) : by_vec(dt, integral_constant<int, kE5M2>{}); };
+    return dtype == kBF16 ? by_fmt(integral_constant<int, kBF16>{}) : by_fmt(integral_constant<int, kF32>{});
+}
+
+static bool rows_fit(const NormLaunch& l, bool vec) { return vec && l.n.group == 0 && l.K == 1; }
+
+// The resident CTAs of the device, or as many as there are rows.
+static cudaError_t rows_grid(const void* kernel, size_t smem, int threads, std::atomic<int>* cache, size_t rows, unsigned& grid) {
+    int dev = 0;
+    cudaError_t err = cudaGetDevice(&dev);
+    if (err != cudaSuccess) return err;
+    if (dev >= kMaxDevices) return cudaErrorInvalidDevice;
+    size_t ctas = 0;
+    err = resident_ctas(kernel, smem, dev, cache, ctas, threads);
+    if (err != cudaSuccess) return err;
+    ctas *= (size_t)sm_count(dev);
+    if (ctas > (size_t)kNorm8Parts) ctas = kNorm8Parts;
+    grid = (unsigned)(ctas < rows ? ctas : rows);
+    return cudaSuccess;
+}
+
+template <typename F>
+static cudaError_t pick_rows(int dtype, int fmt, const NormLaunch& l, F f) {
+    using std::integral_constant;
+    auto by_threads = [&](auto dt, auto fm) {
+        return l.threads <= 256   ? f(dt, fm, integral_constant<int, 256>{})
+               : l.threads <= 320 ? f(dt, fm, integral_constant<int, 320>{})
+               : l.threads <= 384 ? f(dt, fm, integral_constant<int, 384>{})
+               : l.threads <= 512 ? f(dt, fm, integral_constant<int, 512>{})
+                                  : f(dt, fm, integral_constant<int, 1024>{});
+    };
+    auto by_fmt = [&](auto dt) { return fmt == kE4M3 ? by_threads(dt, integral_constant<int, kE4M3>{}) : by_threads(dt, integral_constant<int, kE5M2>{}); };
     return dtype == kBF16 ? by_fmt(integral_constant<int, kBF16>{}) : by_fmt(integral_constant<int, kF32>{});
 }
 
@@ -232,10 +514,30 @@ cudaError_t launch_add_rmsnorm8(const Wide8& x, const Wide8& residual, const voi
                                 const Wide8& out_sum, const Held8& out, const Held8& kept, float* out_rstd, cudaStream_t s) {
     const NormLaunch l = norm_launch(rows, cols, B, dtype);
     const bool vec = wide_vec(x, cols, dtype) && (!residual.p || (wide_vec(residual, cols, dtype) && wide_vec(out_sum, cols, dtype))) && ((uintptr_t)weight & 31) == 0;
-    return pick(dtype, fmt, vec, l, [&](auto dt, auto fm, auto v, auto k, auto small) {
+    if (rows_fit(l, vec)) {
+        return pick_rows(dtype, fmt, l, [&](auto dt, auto fm, auto threads) {
+            auto go = [&](auto res, auto keep) {
+                static std::atomic<int> cache[33][kMaxDevices];   // by the CTA's warps
+                auto* kernel = k_add_rmsnorm8_rows<dt(), fm(), res(), keep(), threads()>;
+                const size_t smem = (size_t)2 * (res() ? 4 : 2) * l.threads * 16;
+                unsigned grid = 0;
+                cudaError_t err = rows_grid((const void*)kernel, smem, (int)l.threads, cache[l.threads / 32], rows, grid);
+                if (err != cudaSuccess) return err;
+                count_launch();
+                const size_t es = dtype == kF32 ? 4 : 2;
+                return launch_pdl(kernel, grid, l.threads, smem, s, (const char*)x.p, x.stride * es, (const char*)residual.p, residual.stride * es, weight, weight_dtype, eps, 1.0f / (float)cols, l.n,
+                                  (char*)out_sum.p, out_sum.stride * es, out, kept, out_rstd);
+            };
+            using Yes = std::integral_constant<bool, true>;
+            using No = std::integral_constant<bool, false>;
+            if (residual.p) return kept.codes ? go(Yes{}, Yes{}) : go(Yes{}, No{});
+            return kept.codes ? go(No{}, Yes{}) : go(No{}, No{});
+        });
+    }
+    return pick(dtype, fmt, vec, l, [&](auto dt, auto fm, auto v, auto k, auto small, auto threads) {
         count_launch();
-        return launch_pdl(k_add_rmsnorm8<dt(), fm(), v(), k(), small()>, (unsigned)((rows + l.rows_cta - 1) / l.rows_cta), l.threads, 0, s, (const void*)x.p, x.stride,
-                          (const void*)residual.p, residual.stride, weight, weight_dtype, eps, l.n, out_sum.p, out_sum.stride, out, kept, out_rstd);
+        return launch_pdl(k_add_rmsnorm8<dt(), fm(), v(), k(), small(), threads()>, (unsigned)((rows + l.rows_cta - 1) / l.rows_cta), l.threads, 0, s, (const void*)x.p, x.stride,
+                          (const void*)residual.p, residual.stride, weight, weight_dtype, eps, 1.0f / (float)cols, l.n, out_sum.p, out_sum.stride, out, kept, out_rstd);
     });
 }
 
@@ -244,20 +546,37 @@ cudaError_t launch_add_rmsnorm8_backward(const Wide8& dy, const Wide8& dsum, con
     const NormLaunch l = norm_launch(rows, cols, B, dtype);
     const bool vec = wide_vec(dy, cols, dtype) && (!dsum.p || wide_vec(dsum, cols, dtype)) && wide_vec(dx, cols, dtype) && ((uintptr_t)weight & 31) == 0 &&
                      (!dweight || ((uintptr_t)parts & 31) == 0);
-    int dev = 0;
-    cudaError_t err = cudaGetDevice(&dev);
-    if (err != cudaSuccess) return err;
-    size_t ctas = (size_t)sm_count(dev) * 2;
-    if (ctas > (rows + l.rows_cta - 1) / l.rows_cta) ctas = (rows + l.rows_cta - 1) / l.rows_cta;
-    if (ctas > (size_t)kNorm8Parts) ctas = kNorm8Parts;
-    err = pick(dtype, fmt, vec, l, [&](auto dt, auto fm, auto v, auto k, auto small) {
-        count_launch();
-        return launch_pdl(k_add_rmsnorm8_backward<dt(), fm(), v(), k(), small()>, (unsigned)ctas, l.threads, 0, s, (const void*)dy.p, dy.stride, (const void*)dsum.p, dsum.stride,
-                          weight, weight_dtype, kept, rstd, l.n, dx.p, dx.stride, dweight ? parts : (float*)nullptr);
-    });
+    unsigned grid = 0;
+    cudaError_t err;
+    if (rows_fit(l, vec)) {
+        err = pick_rows(dtype, fmt, l, [&](auto dt, auto fm, auto threads) {
+            auto go = [&](auto ds) {
+                static std::atomic<int> cache[33][kMaxDevices];   // by the CTA's warps
+                auto* kernel = k_add_rmsnorm8_backward_rows<dt(), fm(), ds(), threads()>;
+                const size_t smem = (size_t)2 * ((ds() ? 5 : 3) * l.threads * 16 + kMeta * l.threads / 8);
+                cudaError_t e = rows_grid((const void*)kernel, smem, (int)l.threads, cache[l.threads / 32], rows, grid);
+                if (e != cudaSuccess) return e;
+                count_launch();
+                const size_t es = dtype == kF32 ? 4 : 2;
+                return launch_pdl(kernel, grid, l.threads, smem, s, (const char*)dy.p, dy.stride * es, (const char*)dsum.p, dsum.stride * es, weight, weight_dtype, kept, rstd,
+                                  1.0f / (float)cols, l.n, (char*)dx.p, dx.stride * es, dweight ? parts : (float*)nullptr);
+            };
+            return dsum.p ? go(std::integral_constant<bool, true>{}) : go(std::integral_constant<bool, false>{});
+        });
+    } else {
+        err = pick(dtype, fmt, vec, l, [&](auto dt, auto fm, auto v, auto k, auto small, auto threads) {
+            static std::atomic<int> cache[33][kMaxDevices];
+            auto* kernel = k_add_rmsnorm8_backward<dt(), fm(), v(), k(), small(), threads()>;
+            cudaError_t e = rows_grid((const void*)kernel, 0, (int)l.threads, cache[l.threads / 32], (rows + l.rows_cta - 1) / l.rows_cta, grid);
+            if (e != cudaSuccess) return e;
+            count_launch();
+            return launch_pdl(kernel, grid, l.threads, 0, s, (const void*)dy.p, dy.stride, (const void*)dsum.p, dsum.stride, weight, weight_dtype, kept, rstd,
+                              1.0f / (float)cols, l.n, dx.p, dx.stride, dweight ? parts : (float*)nullptr);
+        });
+    }
     if (err != cudaSuccess || !dweight) return err;
     count_launch();
-    return launch_pdl(k_rmsnorm8_dweight, (unsigned)((cols + 31) / 32), 256, 0, s, (const float*)parts, (int)ctas, cols, dweight);
+    return launch_pdl(k_rmsnorm8_dweight, (unsigned)((cols + 31) / 32), 1024, 0, s, (const float*)parts, (int)grid, cols, dweight);
 }
 
 }  // namespace mxq
