@@ -41,26 +41,26 @@ static Rows8 rows8(size_t rows, size_t cols, int B, int dtype, bool flat) {
 
 static unsigned grid_of(const Rows8& r) { return (unsigned)((r.rows * r.vectors + kThreads - 1) / kThreads); }
 
-template <int DT, int FMT, bool VEC>
+template <int DT, int FMT, int FIT>
 __global__ void __launch_bounds__(kThreads) k_quantize8(const void* x, size_t stride, Rows8 r, Held8 out) {
     constexpr int V = vec_elems(DT);
     wait_for_prior_grid();
     release_dependents();
     const Place t = r.at<V>((size_t)blockIdx.x * kThreads + threadIdx.x);
     float v[V];
-    load_wide<DT, VEC>(x, t.row * stride + t.vec * V, t.left, v);
-    put_held<FMT, VEC>(out, v, t, r.cols, r.blocks, r.lanes_log2);
+    load_wide<DT, FIT>(x, t.row * stride + t.vec * V, t.left, v);
+    put_held<FMT, FIT>(out, v, t, r.cols, r.blocks, r.lanes_log2);
 }
 
-template <int DT, int FMT, bool VEC>
+template <int DT, int FMT, int FIT>
 __global__ void __launch_bounds__(kThreads) k_dequantize8(Held8 in, Rows8 r, void* out, size_t stride) {
     constexpr int V = vec_elems(DT);
     wait_for_prior_grid();
     release_dependents();
     const Place t = r.at<V>((size_t)blockIdx.x * kThreads + threadIdx.x);
     float v[V];
-    get_held<FMT, VEC>(in, v, t, r.cols, r.blocks, r.lanes_log2);
-    store_wide<DT, VEC>(out, t.row * stride + t.vec * V, t, v);
+    get_held<FMT, FIT>(in, v, t, r.cols, r.blocks, r.lanes_log2);
+    store_wide<DT, FIT>(out, t.row * stride + t.vec * V, t, v);
 }
 
 // 1 / (1 + exp(-g)) of two values.  The reciprocal's argument is 1 at least; where exp(-g) passes 2^126 (g < -87.3) the sigmoid is taken
@@ -83,18 +83,18 @@ __device__ __forceinline__ float2 sigmoid2(float2 g) {
 }
 
 // Registers for five (six) CTAs an SM: 8192 x 14336 with the checkpoints 129 us (four 132, six 140), without 93 with five or six (four 100).
-template <int DT, int FMT, bool VEC, bool KEEP>
-__global__ void __launch_bounds__(kThreads, VEC ? (KEEP ? 5 : 6) : 1) k_swiglu8(const void* gate, size_t gate_stride, const void* up, size_t up_stride, Rows8 r, Held8 out, Held8 out_gate, Held8 out_up) {
+template <int DT, int FMT, int FIT, bool KEEP>
+__global__ void __launch_bounds__(kThreads, FIT != kAny ? (KEEP ? 5 : 6) : 1) k_swiglu8(const void* gate, size_t gate_stride, const void* up, size_t up_stride, Rows8 r, Held8 out, Held8 out_gate, Held8 out_up) {
     constexpr int V = vec_elems(DT);
     wait_for_prior_grid();
     release_dependents();
     const Place t = r.at<V>((size_t)blockIdx.x * kThreads + threadIdx.x);
     float g[V], p[V];
-    load_wide<DT, VEC>(gate, t.row * gate_stride + t.vec * V, t.left, g);
-    load_wide<DT, VEC>(up, t.row * up_stride + t.vec * V, t.left, p);
+    load_wide<DT, FIT>(gate, t.row * gate_stride + t.vec * V, t.left, g);
+    load_wide<DT, FIT>(up, t.row * up_stride + t.vec * V, t.left, p);
     if constexpr (KEEP) {
-        put_held<FMT, VEC>(out_gate, g, t, r.cols, r.blocks, r.lanes_log2);
-        put_held<FMT, VEC>(out_up, p, t, r.cols, r.blocks, r.lanes_log2);
+        put_held<FMT, FIT>(out_gate, g, t, r.cols, r.blocks, r.lanes_log2);
+        put_held<FMT, FIT>(out_up, p, t, r.cols, r.blocks, r.lanes_log2);
     }
 #pragma unroll
     for (int j = 0; j < V; j += 2) {
@@ -102,20 +102,20 @@ __global__ void __launch_bounds__(kThreads, VEC ? (KEEP ? 5 : 6) : 1) k_swiglu8(
         const float2 a = mul2(mul2(gg, sigmoid2<DT>(gg)), make_float2(p[j], p[j + 1]));
         g[j] = a.x, g[j + 1] = a.y;
     }
-    put_held<FMT, VEC>(out, g, t, r.cols, r.blocks, r.lanes_log2);
+    put_held<FMT, FIT>(out, g, t, r.cols, r.blocks, r.lanes_log2);
 }
 
 // Six CTAs an SM: 8192 x 14336 150 us (five 154, four 175).
-template <int DT, int FMT, bool VEC>
-__global__ void __launch_bounds__(kThreads, VEC ? 6 : 1) k_swiglu8_backward(const void* dy, size_t dy_stride, Held8 gate, Held8 up, Rows8 r, void* dgate, size_t dgate_stride, void* dup, size_t dup_stride) {
+template <int DT, int FMT, int FIT>
+__global__ void __launch_bounds__(kThreads, FIT != kAny ? 6 : 1) k_swiglu8_backward(const void* dy, size_t dy_stride, Held8 gate, Held8 up, Rows8 r, void* dgate, size_t dgate_stride, void* dup, size_t dup_stride) {
     constexpr int V = vec_elems(DT);
     wait_for_prior_grid();
     release_dependents();
     const Place t = r.at<V>((size_t)blockIdx.x * kThreads + threadIdx.x);
     float d[V], g[V], p[V];
-    load_wide<DT, VEC>(dy, t.row * dy_stride + t.vec * V, t.left, d);
-    get_held<FMT, VEC>(gate, g, t, r.cols, r.blocks, r.lanes_log2);
-    get_held<FMT, VEC>(up, p, t, r.cols, r.blocks, r.lanes_log2);
+    load_wide<DT, FIT>(dy, t.row * dy_stride + t.vec * V, t.left, d);
+    get_held<FMT, FIT>(gate, g, t, r.cols, r.blocks, r.lanes_log2);
+    get_held<FMT, FIT>(up, p, t, r.cols, r.blocks, r.lanes_log2);
 #pragma unroll
     for (int j = 0; j < V; j += 2) {
         const float2 gg = make_float2(g[j], g[j + 1]), s = sigmoid2<DT>(gg);
@@ -126,40 +126,44 @@ __global__ void __launch_bounds__(kThreads, VEC ? 6 : 1) k_swiglu8_backward(cons
         d[j] = du.x, d[j + 1] = du.y;
         g[j] = dg.x, g[j + 1] = dg.y;
     }
-    store_wide<DT, VEC>(dgate, t.row * dgate_stride + t.vec * V, t, g);
-    store_wide<DT, VEC>(dup, t.row * dup_stride + t.vec * V, t, d);
+    store_wide<DT, FIT>(dgate, t.row * dgate_stride + t.vec * V, t, g);
+    store_wide<DT, FIT>(dup, t.row * dup_stride + t.vec * V, t, d);
 }
 
 template <typename F>
-static cudaError_t pick(int dtype, int fmt, bool vec, F f) {
+static cudaError_t pick(int dtype, int fmt, int fit, F f) {
     using std::integral_constant;
-    auto by_vec = [&](auto dt, auto fm) { return vec ? f(dt, fm, integral_constant<bool, true>{}) : f(dt, fm, integral_constant<bool, false>{}); };
-    auto by_fmt = [&](auto dt) { return fmt == kE4M3 ? by_vec(dt, integral_constant<int, kE4M3>{}) : by_vec(dt, integral_constant<int, kE5M2>{}); };
+    auto by_fit = [&](auto dt, auto fm) {
+        return fit == kWhole  ? f(dt, fm, integral_constant<int, kWhole>{})
+               : fit == kHalf ? f(dt, fm, integral_constant<int, kHalf>{})
+                              : f(dt, fm, integral_constant<int, kAny>{});
+    };
+    auto by_fmt = [&](auto dt) { return fmt == kE4M3 ? by_fit(dt, integral_constant<int, kE4M3>{}) : by_fit(dt, integral_constant<int, kE5M2>{}); };
     return dtype == kBF16 ? by_fmt(integral_constant<int, kBF16>{}) : by_fmt(integral_constant<int, kF32>{});
 }
 
 cudaError_t launch_quantize8(const Wide8& x, size_t rows, size_t cols, int B, int dtype, int fmt, const Held8& out, cudaStream_t s) {
     const Rows8 r = rows8(rows, cols, B, dtype, x.stride == cols && cols % B == 0);
-    return pick(dtype, fmt, wide_vec(x, cols, dtype), [&](auto dt, auto fm, auto vec) {
+    return pick(dtype, fmt, fit_of(x, cols, dtype), [&](auto dt, auto fm, auto fit) {
         count_launch();
-        return launch_pdl(k_quantize8<dt(), fm(), vec()>, grid_of(r), kThreads, 0, s, (const void*)x.p, x.stride, r, out);
+        return launch_pdl(k_quantize8<dt(), fm(), fit()>, grid_of(r), kThreads, 0, s, (const void*)x.p, x.stride, r, out);
     });
 }
 
 cudaError_t launch_dequantize8(const Held8& in, size_t rows, size_t cols, int B, int dtype, int fmt, const Wide8& out, cudaStream_t s) {
     const Rows8 r = rows8(rows, cols, B, dtype, out.stride == cols && cols % B == 0);
-    return pick(dtype, fmt, wide_vec(out, cols, dtype), [&](auto dt, auto fm, auto vec) {
+    return pick(dtype, fmt, fit_of(out, cols, dtype), [&](auto dt, auto fm, auto fit) {
         count_launch();
-        return launch_pdl(k_dequantize8<dt(), fm(), vec()>, grid_of(r), kThreads, 0, s, in, r, out.p, out.stride);
+        return launch_pdl(k_dequantize8<dt(), fm(), fit()>, grid_of(r), kThreads, 0, s, in, r, out.p, out.stride);
     });
 }
 
 cudaError_t launch_swiglu8(const Wide8& gate, const Wide8& up, size_t rows, size_t cols, int B, int dtype, int fmt, const Held8& out, const Held8& out_gate,
                            const Held8& out_up, cudaStream_t s) {
     const Rows8 r = rows8(rows, cols, B, dtype, gate.stride == cols && up.stride == cols && cols % B == 0);
-    return pick(dtype, fmt, wide_vec(gate, cols, dtype) && wide_vec(up, cols, dtype), [&](auto dt, auto fm, auto vec) {
+    return pick(dtype, fmt, worst_fit(fit_of(gate, cols, dtype), fit_of(up, cols, dtype)), [&](auto dt, auto fm, auto fit) {
         count_launch();
-        auto kernel = out_gate.codes ? k_swiglu8<dt(), fm(), vec(), true> : k_swiglu8<dt(), fm(), vec(), false>;
+        auto kernel = out_gate.codes ? k_swiglu8<dt(), fm(), fit(), true> : k_swiglu8<dt(), fm(), fit(), false>;
         return launch_pdl(kernel, grid_of(r), kThreads, 0, s, (const void*)gate.p, gate.stride, (const void*)up.p, up.stride, r, out, out_gate, out_up);
     });
 }
@@ -167,9 +171,9 @@ cudaError_t launch_swiglu8(const Wide8& gate, const Wide8& up, size_t rows, size
 cudaError_t launch_swiglu8_backward(const Wide8& dy, const Held8& gate, const Held8& up, size_t rows, size_t cols, int B, int dtype, int fmt, const Wide8& dgate,
                                     const Wide8& dup, cudaStream_t s) {
     const Rows8 r = rows8(rows, cols, B, dtype, dy.stride == cols && dgate.stride == cols && dup.stride == cols && cols % B == 0);
-    return pick(dtype, fmt, wide_vec(dy, cols, dtype) && wide_vec(dgate, cols, dtype) && wide_vec(dup, cols, dtype), [&](auto dt, auto fm, auto vec) {
+    return pick(dtype, fmt, worst_fit(fit_of(dy, cols, dtype), worst_fit(fit_of(dgate, cols, dtype), fit_of(dup, cols, dtype))), [&](auto dt, auto fm, auto fit) {
         count_launch();
-        return launch_pdl(k_swiglu8_backward<dt(), fm(), vec()>, grid_of(r), kThreads, 0, s, (const void*)dy.p, dy.stride, gate, up, r, dgate.p, dgate.stride, dup.p,
+        return launch_pdl(k_swiglu8_backward<dt(), fm(), fit()>, grid_of(r), kThreads, 0, s, (const void*)dy.p, dy.stride, gate, up, r, dgate.p, dgate.stride, dup.p,
                           dup.stride);
     });
 }

@@ -5,10 +5,10 @@
 // B / 16 or B / 8 neighbouring lanes of one warp, and its maximum takes at most four shuffles.  Rows are padded to whole blocks in
 // this numbering: the lanes behind the end of a row hold zeros and store nothing.
 //
-// Rows that start on 32 bytes and hold whole vectors (VEC) are read and written one vector at a time.  Any other row (an odd number of
-// elements, a view that starts anywhere) is read in the aligned 16-byte pieces that its bytes lie in, shifted into place in
-// registers; on the way out neighbouring lanes exchange what belongs into the other's aligned pieces, and only the two ends of a warp's
-// run are stored element by element.
+// How rows lie (FIT): kWhole, they start on 32 bytes and hold whole vectors, which are read and written at once; kHalf, the same of 16 bytes
+// and half vectors; kAny, all others (an odd number of elements, a view that starts anywhere).  Those are read in the aligned 16-byte
+// pieces that their bytes lie in, shifted into place in registers; on the way out neighbouring lanes exchange what belongs into the
+// other's aligned pieces, and only the two ends of a warp's run are stored element by element.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -51,12 +51,12 @@ __device__ __forceinline__ void store256(void* p, const uint32_t* w) {
                  : "memory");
 }
 
-// NB bytes from p on, of which the first `valid` exist (the others become zeros).  Without VEC the aligned pieces are read whole: a
+// NB bytes from p on, of which the first `valid` exist (the others become zeros).  Under kAny the aligned pieces are read whole: a
 // piece that holds a byte of the row is mapped as a whole.
-template <int NB, bool VEC>
+template <int NB, int FIT>
 __device__ __forceinline__ void load_bytes(const void* p, int valid, uint32_t (&w)[NB / 4]) {
     constexpr int N = NB / 4;
-    if constexpr (VEC) {
+    if constexpr (FIT == kWhole) {
 #pragma unroll
         for (int i = 0; i < N; ++i) w[i] = 0u;
         if (valid <= 0) return;
@@ -69,6 +69,22 @@ __device__ __forceinline__ void load_bytes(const void* p, int valid, uint32_t (&
         } else {
 #pragma unroll
             for (int i = 0; i < N; i += 8) load256(static_cast<const char*>(p) + 4 * i, w + i);
+        }
+    } else if constexpr (FIT == kHalf) {
+        constexpr int G = NB / 2 < 16 ? NB / 2 : 16;
+        const char* q = static_cast<const char*>(p);
+#pragma unroll
+        for (int i = 0; i < NB / G; ++i) {
+            const bool on = i * G < valid;
+            if constexpr (G == 4) {
+                w[i] = on ? *reinterpret_cast<const uint32_t*>(q + 4 * i) : 0u;
+            } else if constexpr (G == 8) {
+                const uint2 a = on ? *reinterpret_cast<const uint2*>(q + 8 * i) : make_uint2(0u, 0u);
+                w[2 * i] = a.x, w[2 * i + 1] = a.y;
+            } else {
+                const uint4 a = on ? *reinterpret_cast<const uint4*>(q + 16 * i) : make_uint4(0u, 0u, 0u, 0u);
+                w[4 * i] = a.x, w[4 * i + 1] = a.y, w[4 * i + 2] = a.z, w[4 * i + 3] = a.w;
+            }
         }
     } else {
         constexpr int G = NB < 16 ? NB : 16, M = N + G / 4;
@@ -102,10 +118,10 @@ __device__ __forceinline__ void load_bytes(const void* p, int valid, uint32_t (&
 
 // NB bytes to p on, of which the first `valid` are stored, in elements of EB bytes.  A warp's lanes hold consecutive vectors, of one row
 // or of several: `first` tells that a vector starts its row, and `after` counts the bytes that its row holds behind it.  All 32 lanes call it.
-template <int NB, int EB, bool VEC>
+template <int NB, int EB, int FIT>
 __device__ __forceinline__ void store_bytes(void* p, int valid, bool first, long long after, const uint32_t (&w)[NB / 4]) {
     constexpr int N = NB / 4;
-    if constexpr (VEC) {
+    if constexpr (FIT == kWhole) {
         if (valid <= 0) return;
         if constexpr (NB == 8) {
             *static_cast<uint2*>(p) = make_uint2(w[0], w[1]);
@@ -114,6 +130,16 @@ __device__ __forceinline__ void store_bytes(void* p, int valid, bool first, long
         } else {
 #pragma unroll
             for (int i = 0; i < N; i += 8) store256(static_cast<char*>(p) + 4 * i, w + i);
+        }
+    } else if constexpr (FIT == kHalf) {
+        constexpr int G = NB / 2 < 16 ? NB / 2 : 16;
+        char* q = static_cast<char*>(p);
+#pragma unroll
+        for (int i = 0; i < NB / G; ++i) {
+            if (i * G >= valid) continue;
+            if constexpr (G == 4) *reinterpret_cast<uint32_t*>(q + 4 * i) = w[i];
+            else if constexpr (G == 8) *reinterpret_cast<uint2*>(q + 8 * i) = make_uint2(w[2 * i], w[2 * i + 1]);
+            else *reinterpret_cast<uint4*>(q + 16 * i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
         }
     } else {
         constexpr int G = NB < 16 ? NB : 16, GW = G / 4, C = NB / G;
@@ -311,34 +337,34 @@ struct Place {
 };
 
 // A wide tensor's vector as fp32.
-template <int DT, bool VEC, int V>
+template <int DT, int FIT, int V>
 __device__ __forceinline__ void load_wide(const void* base, size_t at, long long left, float (&v)[V]) {
     constexpr int EB = elem_bytes(DT);
     uint32_t w[V * EB / 4];
-    load_bytes<V * EB, VEC>(static_cast<const char*>(base) + at * EB, left >= V ? V * EB : (int)left * EB, w);
+    load_bytes<V * EB, FIT>(static_cast<const char*>(base) + at * EB, left >= V ? V * EB : (int)left * EB, w);
     unpack<DT, V>(w, v);
 }
-template <int DT, bool VEC, int V>
+template <int DT, int FIT, int V>
 __device__ __forceinline__ void store_wide(void* base, size_t at, const Place& t, const float (&v)[V]) {
     constexpr int EB = elem_bytes(DT);
     uint32_t w[V * EB / 4];
     pack<DT, V>(v, w);
-    store_bytes<V * EB, EB, VEC>(static_cast<char*>(base) + at * EB, t.left >= V ? V * EB : (int)t.left * EB, t.vec == 0, (t.left - V) * EB, w);
+    store_bytes<V * EB, EB, FIT>(static_cast<char*>(base) + at * EB, t.left >= V ? V * EB : (int)t.left * EB, t.vec == 0, (t.left - V) * EB, w);
 }
 
 // Quantizes and stores this thread's vector; the first lane of a block stores the scale.  The whole warp calls it.
-template <int FMT, bool VEC, int V>
+template <int FMT, int FIT, int V>
 __device__ __forceinline__ void put_held(const Held8& out, const float (&v)[V], const Place& t, size_t cols, size_t blocks, int lanes_log2) {
     uint32_t c[V / 4];
     const uint32_t byte = quantize_block<FMT, V>(v, lanes_log2, c);
-    store_bytes<V, 1, VEC>(out.codes + t.row * cols + t.vec * V, t.left >= V ? V : (int)t.left, t.vec == 0, t.left - V, c);
+    store_bytes<V, 1, FIT>(out.codes + t.row * cols + t.vec * V, t.left >= V ? V : (int)t.left, t.vec == 0, t.left - V, c);
     if (t.left > 0 && (t.vec & (size_t)((1 << lanes_log2) - 1)) == 0) out.scales[t.row * blocks + (t.vec >> lanes_log2)] = (uint8_t)byte;
 }
 
-template <int FMT, bool VEC, int V>
+template <int FMT, int FIT, int V>
 __device__ __forceinline__ void get_held(const Held8& in, float (&v)[V], const Place& t, size_t cols, size_t blocks, int lanes_log2) {
     uint32_t c[V / 4];
-    load_bytes<V, VEC>(in.codes + t.row * cols + t.vec * V, t.left >= V ? V : (int)t.left, c);
+    load_bytes<V, FIT>(in.codes + t.row * cols + t.vec * V, t.left >= V ? V : (int)t.left, c);
     const uint32_t byte = t.left > 0 ? in.scales[t.row * blocks + (t.vec >> lanes_log2)] : 0u;
     dequantize_block<FMT, V>(c, byte, v);
 }

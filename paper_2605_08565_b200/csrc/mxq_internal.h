@@ -136,11 +136,15 @@ struct Wide8 {
     void* p;
     size_t stride;
 };
-// Whether its rows can be read and written in whole vectors of 32 bytes.
-inline bool wide_vec(const Wide8& w, size_t cols, int dtype) {
+// How rows lie: read and written in vectors of 32 bytes, in halves of them, or shifted.
+enum { kAny = 0, kHalf = 1, kWhole = 2 };
+inline int fit_of(const Wide8& w, size_t cols, int dtype) {
     const size_t v = dtype == 0 ? 8 : 16;
-    return (reinterpret_cast<uintptr_t>(w.p) & 31u) == 0 && cols % v == 0 && w.stride % v == 0;
+    const uintptr_t p = reinterpret_cast<uintptr_t>(w.p);
+    if ((p & 31u) == 0 && cols % v == 0 && w.stride % v == 0) return kWhole;
+    return (p & 15u) == 0 && cols % (v / 2) == 0 && w.stride % (v / 2) == 0 ? kHalf : kAny;
 }
+inline int worst_fit(int a, int b) { return a < b ? a : b; }
 constexpr size_t kAct8MaxRows = 0x7FFFFFFF;          // a grid's limit
 constexpr size_t kAct8MaxElems = (size_t)1 << 41;    // rows padded to 128 elements
 constexpr int kNorm8Parts = 1024;         // rows of partial sums in the workspace of the norm's gradient

@@ -46,13 +46,13 @@ __device__ __forceinline__ Place place_of(const NormShape& n, size_t row, int k)
     return t;
 }
 
-template <bool VEC, int V>
+template <int FIT, int V>
 __device__ __forceinline__ void load_weight(const void* weight, int weight_dtype, const Place& t, float (&w)[V]) {
-    if (weight_dtype == kBF16) load_wide<kBF16, VEC>(weight, t.vec * V, t.left, w);
-    else load_wide<kF32, VEC>(weight, t.vec * V, t.left, w);
+    if (weight_dtype == kBF16) load_wide<kBF16, FIT>(weight, t.vec * V, t.left, w);
+    else load_wide<kF32, FIT>(weight, t.vec * V, t.left, w);
 }
 
-template <int DT, int FMT, bool VEC, int K, bool SMALL, int T>
+template <int DT, int FMT, int FIT, int K, bool SMALL, int T>
 __global__ void __launch_bounds__(T) k_add_rmsnorm8(const void* x, size_t x_stride, const void* residual, size_t r_stride, const void* weight, int weight_dtype,
                                                                      float eps, float inv_cols, NormShape n, void* out_sum, size_t s_stride, Held8 out, Held8 kept, float* out_rstd) {
     constexpr int V = vec_elems(DT);
@@ -65,20 +65,20 @@ __global__ void __launch_bounds__(T) k_add_rmsnorm8(const void* x, size_t x_stri
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const Place t = place_of<V, SMALL>(n, row, k);
-        load_wide<DT, VEC>(x, row * x_stride + t.vec * V, t.left, h[k]);
+        load_wide<DT, FIT>(x, row * x_stride + t.vec * V, t.left, h[k]);
         if (residual) {
             float r[V];
-            load_wide<DT, VEC>(residual, row * r_stride + t.vec * V, t.left, r);
+            load_wide<DT, FIT>(residual, row * r_stride + t.vec * V, t.left, r);
 #pragma unroll
             for (int j = 0; j < V; ++j) h[k][j] += r[j];
             uint32_t w[V * elem_bytes(DT) / 4];
             pack<DT, V>(h[k], w);
             unpack<DT, V>(w, h[k]);
-            store_wide<DT, VEC>(out_sum, row * s_stride + t.vec * V, t, h[k]);
+            store_wide<DT, FIT>(out_sum, row * s_stride + t.vec * V, t, h[k]);
         }
 #pragma unroll
         for (int j = 0; j < V; ++j) sq = __fmaf_rn(h[k][j], h[k][j], sq);
-        if (kept.codes) put_held<FMT, VEC>(kept, h[k], t, n.cols, n.blocks, n.lanes_log2);
+        if (kept.codes) put_held<FMT, FIT>(kept, h[k], t, n.cols, n.blocks, n.lanes_log2);
     }
     sq = row_sum<SMALL>(sq, n.group, scratch);
     const float rstd = rsqrtf(__fmaf_rn(sq, inv_cols, eps));
@@ -87,19 +87,19 @@ __global__ void __launch_bounds__(T) k_add_rmsnorm8(const void* x, size_t x_stri
         const Place t = place_of<V, SMALL>(n, row, k);
         if (out_rstd && t.vec == 0 && row < n.rows) out_rstd[row] = rstd;
         float w[V];
-        load_weight<VEC, V>(weight, weight_dtype, t, w);
+        load_weight<FIT, V>(weight, weight_dtype, t, w);
 #pragma unroll
         for (int j = 0; j < V; j += 2) {
             const float2 y = mul2(mul2(make_float2(h[k][j], h[k][j + 1]), make_float2(rstd, rstd)), make_float2(w[j], w[j + 1]));
             w[j] = y.x, w[j + 1] = y.y;
         }
-        put_held<FMT, VEC>(out, w, t, n.cols, n.blocks, n.lanes_log2);
+        put_held<FMT, FIT>(out, w, t, n.cols, n.blocks, n.lanes_log2);
     }
 }
 
 // A CTA takes every gridDim.x-th row (or group of rows); a thread holds the same K vectors of each and adds up its columns' part of the
 // weight's gradient.
-template <int DT, int FMT, bool VEC, int K, bool SMALL, int T>
+template <int DT, int FMT, int FIT, int K, bool SMALL, int T>
 __global__ void __launch_bounds__(T) k_add_rmsnorm8_backward(const void* dy, size_t dy_stride, const void* dsum, size_t ds_stride, const void* weight,
                                                                               int weight_dtype, Held8 kept, const float* rstd, float inv_cols, NormShape n, void* dx, size_t dx_stride,
                                                                               float* parts) {
@@ -123,10 +123,10 @@ __global__ void __launch_bounds__(T) k_add_rmsnorm8_backward(const void* dy, siz
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const Place t = place_of<V, SMALL>(n, row, k);
-            load_wide<DT, VEC>(dy, row * dy_stride + t.vec * V, t.left, wd[k]);
-            get_held<FMT, VEC>(kept, xh[k], t, n.cols, n.blocks, n.lanes_log2);
+            load_wide<DT, FIT>(dy, row * dy_stride + t.vec * V, t.left, wd[k]);
+            get_held<FMT, FIT>(kept, xh[k], t, n.cols, n.blocks, n.lanes_log2);
             float w[V];
-            load_weight<VEC, V>(weight, weight_dtype, t, w);
+            load_weight<FIT, V>(weight, weight_dtype, t, w);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 xh[k][j] *= rs;
@@ -140,13 +140,13 @@ __global__ void __launch_bounds__(T) k_add_rmsnorm8_backward(const void* dy, siz
         for (int k = 0; k < K; ++k) {
             const Place t = place_of<V, SMALL>(n, row, k);
             float ds[V];
-            if (dsum) load_wide<DT, VEC>(dsum, row * ds_stride + t.vec * V, t.left, ds);
+            if (dsum) load_wide<DT, FIT>(dsum, row * ds_stride + t.vec * V, t.left, ds);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const float e = __fmaf_rn(-xh[k][j], c, wd[k][j]);
                 wd[k][j] = dsum ? __fmaf_rn(e, rs, ds[j]) : e * rs;
             }
-            store_wide<DT, VEC>(dx, row * dx_stride + t.vec * V, t, wd[k]);
+            store_wide<DT, FIT>(dx, row * dx_stride + t.vec * V, t, wd[k]);
         }
     }
     if (!parts) return;
@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(T) k_add_rmsnorm8_backward(const void* dy, siz
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const Place t = place_of<V, SMALL>(n, 0, k);
-            store_wide<kF32, VEC>(parts, blockIdx.x * n.cols + t.vec * V, t, dw[k]);
+            store_wide<kF32, FIT>(parts, blockIdx.x * n.cols + t.vec * V, t, dw[k]);
         }
     }
 }
@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(T, T == 256 ? (RES ? 2 : 3) : T <= 384 ? 2 : 1
     if constexpr (RES) copy(slot + 2 * n_thr, pr);
     copy_commit();
     float w[V];
-    load_weight<true, V>(weight, weight_dtype, t, w);
+    load_weight<kWhole, V>(weight, weight_dtype, t, w);
     __syncthreads();   // the zeros in `sums`
     for (int turn = 0; row < n.rows; row += step, turn ^= 1) {
         __syncwarp();   // the other lanes have read what the next copies replace
@@ -345,7 +345,7 @@ __global__ void __launch_bounds__(T, T <= 320 ? 2 : 1)
     fetch(slot);
     copy_commit();
     float w[V], dw[V];
-    load_weight<true, V>(weight, weight_dtype, t, w);
+    load_weight<kWhole, V>(weight, weight_dtype, t, w);
 #pragma unroll
     for (int j = 0; j < V; ++j) dw[j] = 0.0f;
     __syncthreads();   // the zeros in `sums`
@@ -462,37 +462,60 @@ static NormLaunch norm_launch(size_t rows, size_t cols, int B, int dtype) {
 }
 
 template <typename F>
-static cudaError_t pick(int dtype, int fmt, bool vec, const NormLaunch& l, F f) {
+static cudaError_t pick(int dtype, int fmt, int fit, const NormLaunch& l, F f) {
     using std::integral_constant;
     using Yes = integral_constant<bool, true>;
     using No = integral_constant<bool, false>;
-    auto by_k = [&](auto dt, auto fm, auto v) {
-        if (l.n.group) return f(dt, fm, v, integral_constant<int, 1>{}, Yes{}, integral_constant<int, 256>{});
-        if (l.K == 1 && l.threads <= 256) return f(dt, fm, v, integral_constant<int, 1>{}, No{}, integral_constant<int, 256>{});
-        if (l.K == 1 && l.threads <= 512) return f(dt, fm, v, integral_constant<int, 1>{}, No{}, integral_constant<int, 512>{});
-        return l.K == 1   ? f(dt, fm, v, integral_constant<int, 1>{}, No{}, integral_constant<int, 1024>{})
-               : l.K == 2 ? f(dt, fm, v, integral_constant<int, 2>{}, No{}, integral_constant<int, 1024>{})
-                          : f(dt, fm, v, integral_constant<int, 4>{}, No{}, integral_constant<int, 1024>{});
+    auto by_k = [&](auto dt, auto fm, auto fit) {
+        if (l.n.group) return f(dt, fm, fit, integral_constant<int, 1>{}, Yes{}, integral_constant<int, 256>{});
+        if constexpr (fit() != kWhole) {   // those are rows_fit()
+            if (l.K == 1 && l.threads <= 256) return f(dt, fm, fit, integral_constant<int, 1>{}, No{}, integral_constant<int, 256>{});
+            if (l.K == 1 && l.threads <= 512) return f(dt, fm, fit, integral_constant<int, 1>{}, No{}, integral_constant<int, 512>{});
+            if (l.K == 1) return f(dt, fm, fit, integral_constant<int, 1>{}, No{}, integral_constant<int, 1024>{});
+        }
+        return l.K == 2 ? f(dt, fm, fit, integral_constant<int, 2>{}, No{}, integral_constant<int, 1024>{})
+                        : f(dt, fm, fit, integral_constant<int, 4>{}, No{}, integral_constant<int, 1024>{});
     };
-    auto by_vec = [&](auto dt, auto fm) { return vec ? by_k(dt, fm, Yes{}) : by_k(dt, fm, No{}); };
-    auto by_fmt = [&](auto dt) { return fmt == kE4M3 ? by_vec(dt, integral_constant<int, kE4M3>{}) : by_vec(dt, integral_constant<int, kE5M2>{}); };
+    auto by_fit = [&](auto dt, auto fm) {
+        return fit == kWhole  ? by_k(dt, fm, integral_constant<int, kWhole>{})
+               : fit == kHalf ? by_k(dt, fm, integral_constant<int, kHalf>{})
+                              : by_k(dt, fm, integral_constant<int, kAny>{});
+    };
+    auto by_fmt = [&](auto dt) { return fmt == kE4M3 ? by_fit(dt, integral_constant<int, kE4M3>{}) : by_fit(dt, integral_constant<int, kE5M2>{}); };
     return dtype == kBF16 ? by_fmt(integral_constant<int, kBF16>{}) : by_fmt(integral_constant<int, kF32>{});
 }
 
-static bool rows_fit(const NormLaunch& l, bool vec) { return vec && l.n.group == 0 && l.K == 1; }
+static bool rows_fit(const NormLaunch& l, int fit) { return fit == kWhole && l.n.group == 0 && l.K == 1; }
 
-// The resident CTAs of the device, or as many as there are rows.
-static cudaError_t rows_grid(const void* kernel, size_t smem, int threads, std::atomic<int>* cache, size_t rows, unsigned& grid) {
+// A vector of cols elements that goes with rows of `dtype`: pieces of as many elements as theirs.
+static int fit_of_weight(const void* p, int weight_dtype, int dtype, size_t cols) {
+    const size_t v = (size_t)vec_elems(dtype);
+    const uintptr_t bytes = v * (weight_dtype == kF32 ? 4 : 2), at = reinterpret_cast<uintptr_t>(p);   // of a vector: 16, 32 or 64
+    const uintptr_t whole = bytes < 32 ? bytes : 32, half = bytes / 2 < 16 ? bytes / 2 : 16;
+    if (at % whole == 0 && cols % v == 0) return kWhole;
+    return at % half == 0 && cols % (v / 2) == 0 ? kHalf : kAny;
+}
+
+// Grid of a kernel whose CTAs take turns on `work` rows (or groups of rows): the resident CTAs of the device, `most` at most.  smem: of this launch;
+// smem_most: of the kernel's largest, which its limit has to allow whatever launch comes first.  cache: one for each number of warps.
+static cudaError_t rows_grid(const void* kernel, size_t smem, size_t smem_most, unsigned threads, std::atomic<int> (*cache)[kMaxDevices], size_t work, size_t most,
+                             unsigned& grid) {
     int dev = 0;
     cudaError_t err = cudaGetDevice(&dev);
     if (err != cudaSuccess) return err;
     if (dev >= kMaxDevices) return cudaErrorInvalidDevice;
-    size_t ctas = 0;
-    err = resident_ctas(kernel, smem, dev, cache, ctas, threads);
-    if (err != cudaSuccess) return err;
-    ctas *= (size_t)sm_count(dev);
-    if (ctas > (size_t)kNorm8Parts) ctas = kNorm8Parts;
-    grid = (unsigned)(ctas < rows ? ctas : rows);
+    int ctas = cache[threads / 32][dev].load(std::memory_order_relaxed);
+    if (ctas == 0) {   // threads that race here store the same value
+        err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_most);
+        if (err != cudaSuccess) return err;
+        err = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ctas, kernel, (int)threads, smem);
+        if (err != cudaSuccess) return err;
+        if (ctas < 1) ctas = 1;
+        cache[threads / 32][dev].store(ctas, std::memory_order_relaxed);
+    }
+    size_t g = (size_t)ctas * (size_t)sm_count(dev);
+    if (g > most) g = most;
+    grid = (unsigned)(g < work ? g : work);
     return cudaSuccess;
 }
 
@@ -513,15 +536,17 @@ static cudaError_t pick_rows(int dtype, int fmt, const NormLaunch& l, F f) {
 cudaError_t launch_add_rmsnorm8(const Wide8& x, const Wide8& residual, const void* weight, int weight_dtype, size_t rows, size_t cols, float eps, int B, int dtype, int fmt,
                                 const Wide8& out_sum, const Held8& out, const Held8& kept, float* out_rstd, cudaStream_t s) {
     const NormLaunch l = norm_launch(rows, cols, B, dtype);
-    const bool vec = wide_vec(x, cols, dtype) && (!residual.p || (wide_vec(residual, cols, dtype) && wide_vec(out_sum, cols, dtype))) && ((uintptr_t)weight & 31) == 0;
-    if (rows_fit(l, vec)) {
+    int fit = worst_fit(fit_of(x, cols, dtype), fit_of_weight(weight, weight_dtype, dtype, cols));
+    if (residual.p) fit = worst_fit(fit, worst_fit(fit_of(residual, cols, dtype), fit_of(out_sum, cols, dtype)));
+    if (rows_fit(l, fit)) {
         return pick_rows(dtype, fmt, l, [&](auto dt, auto fm, auto threads) {
             auto go = [&](auto res, auto keep) {
-                static std::atomic<int> cache[33][kMaxDevices];   // by the CTA's warps
+                static std::atomic<int> cache[33][kMaxDevices];
                 auto* kernel = k_add_rmsnorm8_rows<dt(), fm(), res(), keep(), threads()>;
-                const size_t smem = (size_t)2 * (res() ? 4 : 2) * l.threads * 16;
+                auto smem_of = [&](size_t n) { return 2 * (res() ? 4 : 2) * n * 16; };
+                const size_t smem = smem_of(l.threads);
                 unsigned grid = 0;
-                cudaError_t err = rows_grid((const void*)kernel, smem, (int)l.threads, cache[l.threads / 32], rows, grid);
+                cudaError_t err = rows_grid((const void*)kernel, smem, smem_of(threads()), l.threads, cache, rows, SIZE_MAX, grid);
                 if (err != cudaSuccess) return err;
                 count_launch();
                 const size_t es = dtype == kF32 ? 4 : 2;
@@ -534,7 +559,7 @@ cudaError_t launch_add_rmsnorm8(const Wide8& x, const Wide8& residual, const voi
             return kept.codes ? go(No{}, Yes{}) : go(No{}, No{});
         });
     }
-    return pick(dtype, fmt, vec, l, [&](auto dt, auto fm, auto v, auto k, auto small, auto threads) {
+    return pick(dtype, fmt, fit, l, [&](auto dt, auto fm, auto v, auto k, auto small, auto threads) {
         count_launch();
         return launch_pdl(k_add_rmsnorm8<dt(), fm(), v(), k(), small(), threads()>, (unsigned)((rows + l.rows_cta - 1) / l.rows_cta), l.threads, 0, s, (const void*)x.p, x.stride,
                           (const void*)residual.p, residual.stride, weight, weight_dtype, eps, 1.0f / (float)cols, l.n, out_sum.p, out_sum.stride, out, kept, out_rstd);
@@ -544,17 +569,19 @@ cudaError_t launch_add_rmsnorm8(const Wide8& x, const Wide8& residual, const voi
 cudaError_t launch_add_rmsnorm8_backward(const Wide8& dy, const Wide8& dsum, const void* weight, int weight_dtype, const Held8& kept, const float* rstd, size_t rows, size_t cols,
                                          int B, int dtype, int fmt, const Wide8& dx, float* dweight, float* parts, cudaStream_t s) {
     const NormLaunch l = norm_launch(rows, cols, B, dtype);
-    const bool vec = wide_vec(dy, cols, dtype) && (!dsum.p || wide_vec(dsum, cols, dtype)) && wide_vec(dx, cols, dtype) && ((uintptr_t)weight & 31) == 0 &&
-                     (!dweight || ((uintptr_t)parts & 31) == 0);
+    int fit = worst_fit(worst_fit(fit_of(dy, cols, dtype), fit_of(dx, cols, dtype)), fit_of_weight(weight, weight_dtype, dtype, cols));
+    if (dsum.p) fit = worst_fit(fit, fit_of(dsum, cols, dtype));
+    if (dweight) fit = worst_fit(fit, fit_of_weight(parts, kF32, dtype, cols));
     unsigned grid = 0;
     cudaError_t err;
-    if (rows_fit(l, vec)) {
+    if (rows_fit(l, fit)) {
         err = pick_rows(dtype, fmt, l, [&](auto dt, auto fm, auto threads) {
             auto go = [&](auto ds) {
-                static std::atomic<int> cache[33][kMaxDevices];   // by the CTA's warps
+                static std::atomic<int> cache[33][kMaxDevices];
                 auto* kernel = k_add_rmsnorm8_backward_rows<dt(), fm(), ds(), threads()>;
-                const size_t smem = (size_t)2 * ((ds() ? 5 : 3) * l.threads * 16 + kMeta * l.threads / 8);
-                cudaError_t e = rows_grid((const void*)kernel, smem, (int)l.threads, cache[l.threads / 32], rows, grid);
+                auto smem_of = [&](size_t n) { return 2 * ((ds() ? 5 : 3) * n * 16 + kMeta * n / 8); };
+                const size_t smem = smem_of(l.threads);
+                cudaError_t e = rows_grid((const void*)kernel, smem, smem_of(threads()), l.threads, cache, rows, kNorm8Parts, grid);
                 if (e != cudaSuccess) return e;
                 count_launch();
                 const size_t es = dtype == kF32 ? 4 : 2;
@@ -564,10 +591,10 @@ cudaError_t launch_add_rmsnorm8_backward(const Wide8& dy, const Wide8& dsum, con
             return dsum.p ? go(std::integral_constant<bool, true>{}) : go(std::integral_constant<bool, false>{});
         });
     } else {
-        err = pick(dtype, fmt, vec, l, [&](auto dt, auto fm, auto v, auto k, auto small, auto threads) {
+        err = pick(dtype, fmt, fit, l, [&](auto dt, auto fm, auto v, auto k, auto small, auto threads) {
             static std::atomic<int> cache[33][kMaxDevices];
             auto* kernel = k_add_rmsnorm8_backward<dt(), fm(), v(), k(), small(), threads()>;
-            cudaError_t e = rows_grid((const void*)kernel, 0, (int)l.threads, cache[l.threads / 32], (rows + l.rows_cta - 1) / l.rows_cta, grid);
+            cudaError_t e = rows_grid((const void*)kernel, 0, 0, l.threads, cache, (rows + l.rows_cta - 1) / l.rows_cta, kNorm8Parts, grid);
             if (e != cudaSuccess) return e;
             count_launch();
             return launch_pdl(kernel, grid, l.threads, 0, s, (const void*)dy.p, dy.stride, (const void*)dsum.p, dsum.stride, weight, weight_dtype, kept, rstd,

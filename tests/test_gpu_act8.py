@@ -87,7 +87,8 @@ def check_exact(c, s, x, B, fmt, cols):
     assert c.untouched() and s.untouched()
 
 
-SHAPES = [(1, 1, 0, 0), (1, 16, 0, 0), (3, 40, 0, 0), (5, 129, 0, 0), (2, 4096, 0, 0), (7, 1000, 8, 0), (33, 264, 3, 0), (300, 72, 0, 1), (1, 70001, 0, 0), (513, 8, 0, 8)]
+SHAPES = [(1, 1, 0, 0), (1, 16, 0, 0), (3, 40, 0, 0), (5, 129, 0, 0), (2, 4096, 0, 0), (7, 1000, 8, 0), (33, 264, 3, 0), (300, 72, 0, 1), (1, 70001, 0, 0), (513, 8, 0, 8), (9, 132, 4, 0),
+          (5, 2052, 0, 4)]
 
 
 @pytest.mark.parametrize("B", [16, 32, 64, 128])
@@ -124,7 +125,7 @@ def test_dequantize8_is_exact(rows, cols, pad, shift, dtype, fmt, B):
 
 # Rows of one and of several vectors a thread, of whole and short blocks, on and off the 16-byte grid; more rows than resident CTAs.
 NORM_SHAPES = [(1, 1, 0, 0), (1, 4096, 0, 0), (3, 40, 0, 0), (5, 129, 0, 0), (7, 1000, 8, 0), (33, 264, 3, 0), (700, 72, 0, 0), (1300, 520, 0, 1), (3, 5120, 0, 0),
-               (2, 8200, 0, 0), (2, 16392, 8, 0), (2, 32768, 0, 0), (2, 16385, 0, 0), (2, 32767, 1, 0)]
+               (2, 8200, 0, 0), (2, 16392, 8, 0), (2, 32768, 0, 0), (2, 16385, 0, 0), (2, 32767, 1, 0), (3, 2052, 0, 0), (2, 6144, 0, 0), (2, 8192, 16, 0), (2, 16384, 0, 0), (2500, 544, 0, 0)]
 
 
 def rel_of_norm(cols):
@@ -173,6 +174,29 @@ def test_add_rmsnorm8(rows, cols, pad, shift, fmt, B, dtype, wdtype, with_residu
     c2, s2 = held_out(rows, cols, B)
     mxq.mxq_add_rmsnorm8(x, r, w, eps, B, fmt, total.t if total else None, c2.t, s2.t)
     assert torch.equal(c2.t, c.t) and torch.equal(s2.t, s.t)
+
+
+def test_norms_of_more_rows_than_the_device_holds():
+    """Every CTA comes to several rows of 4096 elements, forward and backward."""
+    rows, cols, B = 1000, 4096, 32
+    x, r, w = norm_inputs(rows, cols, 0, 0, BF16, BF16, 1)
+    total = torch.empty_like(x)
+    (c, s), (kc, ks) = held_out(rows, cols, B), held_out(rows, cols, B)
+    rstd = torch.empty(rows, device="cuda")
+    mxq.mxq_add_rmsnorm8(x, r, w, 1e-5, B, ref.E4M3, total, c.t, s.t, kc.t, ks.t, rstd)
+    h = np64(total)
+    assert torch.equal(total, (x.float() + r.float()).to(BF16))
+    check_exact(kc, ks, h, B, ref.E4M3, cols)
+    y = ref.rmsnorm(h, np64(w), np.float64(np.float32(1e-5)))[0]
+    ref.check_held(c.t.cpu().numpy().reshape(rows, cols), s.t.cpu().numpy().reshape(rows, -1), y, rel_of_norm(cols), B, ref.E4M3)
+    dy = Guarded(rows, cols, BF16).fill((torch.randn(rows, cols, generator=torch.Generator().manual_seed(2)) * 1e-3).to(BF16))
+    dx, dw = Guarded(rows, cols, BF16), Guarded(1, cols, F32)
+    mxq.mxq_add_rmsnorm8_backward(dy, r, w, kc.t.view(rows, cols), ks.t.view(rows, -1), rstd, B, ref.E4M3, dx.t, dw.t, workspace(rows, cols))
+    held = ref.dequantize(kc.t.cpu().numpy().reshape(rows, cols), ks.t.cpu().numpy().reshape(rows, -1), B, ref.E4M3)
+    wx, ww, size, wsize = ref.rmsnorm_backward(np64(dy), np64(w), held, np64(rstd), np64(r))
+    assert (np.abs(np64(dx.t) - wx) <= HALF[BF16] * np.abs(wx) + 65 * U * size).all()
+    assert (np.abs(np64(dw.t)[0] - ww) <= (rows + 3) * U * wsize).all()
+    assert dx.untouched() and dw.untouched()
 
 
 def test_add_rmsnorm8_in_place():
@@ -265,7 +289,7 @@ def gated_inputs(rows, cols, dtype, halves, seed, pad=0, shift=0):
 
 
 GATED_SHAPES = [(1, 1, False, 0, 0), (1, 14336, True, 0, 0), (3, 40, True, 0, 0), (5, 129, True, 0, 0), (7, 1000, False, 8, 0), (33, 264, False, 3, 0), (300, 72, True, 0, 0),
-                (65, 2730, False, 0, 0), (9, 2048, False, 0, 1)]
+                (65, 2730, False, 0, 0), (9, 2048, False, 0, 1), (9, 132, True, 0, 0), (5, 2052, False, 4, 0)]
 
 
 def off_of_sigmoid(g, dtype):
