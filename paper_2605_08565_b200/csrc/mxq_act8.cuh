@@ -26,17 +26,29 @@ constexpr unsigned kFull = 0xFFFFFFFFu;
 __host__ __device__ constexpr int vec_elems(int dt) { return dt == kF32 ? 8 : 16; }
 
 // ---- bytes ---------------------------------------------------------------------------------------
-// w = the words of c from byte `by` (< 4 * (M - N)) on.
-template <int N, int M>
-__device__ __forceinline__ void shift_down(uint32_t (&c)[M], unsigned by, uint32_t (&w)[N]) {
-    if constexpr (M - N > 2) {
+// w = the words of c from byte `by` (< 4 * (M - N)) on; EB: by is a multiple of it.  `by` is the same for all vectors of a row, so that the
+// branch is one of the whole warp but for its row ends; selecting every word by two bits of it instead made the shifted rows wait for the
+// ALU (four fifths busy).
+template <int EB, int Q, int N, int M>
+__device__ __forceinline__ void words_from(const uint32_t (&c)[M], unsigned by, uint32_t (&w)[N]) {
 #pragma unroll
-        for (int i = 0; i + 2 < M; ++i) c[i] = by & 8u ? c[i + 2] : c[i];
+    for (int i = 0; i < N; ++i) {
+        if constexpr (EB == 4) w[i] = c[i + Q];
+        else w[i] = __funnelshift_r(c[i + Q], c[i + Q + 1 < M ? i + Q + 1 : i + Q], 8u * (by & 3u));
     }
-#pragma unroll
-    for (int i = 0; i + 1 < M; ++i) c[i] = by & 4u ? c[i + 1] : c[i];
-#pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = __funnelshift_r(c[i], c[i + 1 < M ? i + 1 : i], 8u * (by & 3u));
+}
+template <int EB, int N, int M>
+__device__ __forceinline__ void shift_down(const uint32_t (&c)[M], unsigned by, uint32_t (&w)[N]) {
+    switch (by >> 2) {
+    case 0: words_from<EB, 0>(c, by, w); break;
+    case 1: words_from<EB, 1>(c, by, w); break;
+    case 2:
+        if constexpr (M - N > 2) words_from<EB, 2>(c, by, w);
+        break;
+    default:
+        if constexpr (M - N > 2) words_from<EB, 3>(c, by, w);
+        break;
+    }
 }
 
 __device__ __forceinline__ void load256(const void* p, uint32_t* w) {
@@ -51,9 +63,9 @@ __device__ __forceinline__ void store256(void* p, const uint32_t* w) {
                  : "memory");
 }
 
-// NB bytes from p on, of which the first `valid` exist (the others become zeros).  Under kAny the aligned pieces are read whole: a
+// NB bytes from p on, of which the first `valid` exist (the others become zeros), in elements of EB bytes.  Under kAny the aligned pieces are read whole: a
 // piece that holds a byte of the row is mapped as a whole.
-template <int NB, int FIT>
+template <int NB, int EB, int FIT>
 __device__ __forceinline__ void load_bytes(const void* p, int valid, uint32_t (&w)[NB / 4]) {
     constexpr int N = NB / 4;
     if constexpr (FIT == kWhole) {
@@ -105,7 +117,7 @@ __device__ __forceinline__ void load_bytes(const void* p, int valid, uint32_t (&
                 }
             }
         }
-        shift_down<N, M>(c, by, w);
+        shift_down<EB>(c, by, w);
         if (valid < NB) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -114,6 +126,13 @@ __device__ __forceinline__ void load_bytes(const void* p, int valid, uint32_t (&
             }
         }
     }
+}
+
+template <int EB>
+__device__ __forceinline__ void store_element(char* to, uint32_t v) {
+    if constexpr (EB == 4) *reinterpret_cast<uint32_t*>(to) = v;
+    else if constexpr (EB == 2) *reinterpret_cast<uint16_t*>(to) = (uint16_t)v;
+    else *reinterpret_cast<uint8_t*>(to) = (uint8_t)v;
 }
 
 // NB bytes to p on, of which the first `valid` are stored, in elements of EB bytes.  A warp's lanes hold consecutive vectors, of one row
@@ -151,7 +170,7 @@ __device__ __forceinline__ void store_bytes(void* p, int valid, bool first, long
 #pragma unroll
         for (int i = 0; i < GW; ++i) c[N + i] = __shfl_down_sync(kFull, w[i], 1);
         uint32_t out[N];
-        shift_down<N, N + GW>(c, (unsigned)h, out);
+        shift_down<EB>(c, (unsigned)h, out);
         if (valid <= 0) return;
         const bool head_taken = h == 0 || (lane > 0 && !first && valid >= h);   // by the lane before
         const bool last_whole = valid == NB && (h == 0 || (lane < 31 && after >= h));
@@ -165,16 +184,41 @@ __device__ __forceinline__ void store_bytes(void* p, int valid, bool first, long
                 done += G;
             }
         }
-        if (!head_taken || done < valid) {
+        if (!head_taken) {   // the first h bytes, in pieces of 1, 2, 4 and 8 up to the first aligned address
+            char* to = static_cast<char*>(p);
+            if (valid < h) {   // a short vector that does not come so far
 #pragma unroll
-            for (int b = 0; b < NB; b += EB) {
-                if (b < valid && (b >= done || (b < h && !head_taken))) {
-                    char* to = static_cast<char*>(p) + b;
-                    if constexpr (EB == 4) *reinterpret_cast<uint32_t*>(to) = w[b / 4];
-                    else if constexpr (EB == 2) *reinterpret_cast<uint16_t*>(to) = (uint16_t)(w[b / 4] >> (8 * (b & 3)));
-                    else *reinterpret_cast<uint8_t*>(to) = (uint8_t)(w[b / 4] >> (8 * (b & 3)));
+                for (int b = 0; b < G; b += EB)
+                    if (b < valid) store_element<EB>(to + b, w[b / 4] >> (8 * (b & 3)));
+            } else {
+                const unsigned sh = 8u * (h & 3);
+                if (EB <= 1 && (h & 1)) store_element<1>(to, w[0]);
+                if (EB <= 2 && (h & 2)) store_element<2>(to + (h & 1), w[0] >> (8 * (h & 1)));
+                if (h & 4) store_element<4>(to + (h & 3), __funnelshift_r(w[0], w[1], sh));
+                if constexpr (G == 16) {
+                    if (h & 8) {
+                        const bool q = h & 4;
+                        const uint32_t a0 = q ? w[1] : w[0], a1 = q ? w[2] : w[1], a2 = q ? w[3] : w[2];
+                        *reinterpret_cast<uint2*>(to + (h & 7)) = make_uint2(__funnelshift_r(a0, a1, sh), __funnelshift_r(a1, a2, sh));
+                    }
                 }
             }
+        }
+        if (done < valid) {   // the last bytes, from an aligned address on, in pieces of 8, 4, 2 and 1
+            char* to = static_cast<char*>(p) + done;
+            const int n = valid - done;
+            uint32_t t[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int i = 0; i < C; ++i)
+#pragma unroll
+                for (int k = 0; k < GW; ++k) t[k] = done == h + i * G ? out[i * GW + k] : t[k];
+            if constexpr (G == 16)
+                if (n & 8) *reinterpret_cast<uint2*>(to) = make_uint2(t[0], t[1]);
+            const uint32_t t4 = n & 8 ? t[2] : t[0], t5 = n & 8 ? t[3] : t[1];
+            if (n & 4) store_element<4>(to + (n & 8), t4);
+            const uint32_t t2 = n & 4 ? t5 : t4;
+            if (EB <= 2 && (n & 2)) store_element<2>(to + (n & 12), t2);
+            if (EB <= 1 && (n & 1)) store_element<1>(to + (n & 14), t2 >> (8 * (n & 2)));
         }
     }
 }
@@ -231,6 +275,8 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
     asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(z));
     return r;
 }
+
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 // ---- asynchronous copies into shared memory: a thread reads back only what it copied itself ----
 __device__ __forceinline__ void copy_async16(void* to, const void* from) {
@@ -341,7 +387,7 @@ template <int DT, int FIT, int V>
 __device__ __forceinline__ void load_wide(const void* base, size_t at, long long left, float (&v)[V]) {
     constexpr int EB = elem_bytes(DT);
     uint32_t w[V * EB / 4];
-    load_bytes<V * EB, FIT>(static_cast<const char*>(base) + at * EB, left >= V ? V * EB : (int)left * EB, w);
+    load_bytes<V * EB, EB, FIT>(static_cast<const char*>(base) + at * EB, left >= V ? V * EB : (int)left * EB, w);
     unpack<DT, V>(w, v);
 }
 template <int DT, int FIT, int V>
@@ -364,7 +410,7 @@ __device__ __forceinline__ void put_held(const Held8& out, const float (&v)[V], 
 template <int FMT, int FIT, int V>
 __device__ __forceinline__ void get_held(const Held8& in, float (&v)[V], const Place& t, size_t cols, size_t blocks, int lanes_log2) {
     uint32_t c[V / 4];
-    load_bytes<V, FIT>(in.codes + t.row * cols + t.vec * V, t.left >= V ? V : (int)t.left, c);
+    load_bytes<V, 1, FIT>(in.codes + t.row * cols + t.vec * V, t.left >= V ? V : (int)t.left, c);
     const uint32_t byte = t.left > 0 ? in.scales[t.row * blocks + (t.vec >> lanes_log2)] : 0u;
     dequantize_block<FMT, V>(c, byte, v);
 }

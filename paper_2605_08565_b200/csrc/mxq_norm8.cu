@@ -53,7 +53,7 @@ __device__ __forceinline__ void load_weight(const void* weight, int weight_dtype
 }
 
 template <int DT, int FMT, int FIT, int K, bool SMALL, int T>
-__global__ void __launch_bounds__(T) k_add_rmsnorm8(const void* x, size_t x_stride, const void* residual, size_t r_stride, const void* weight, int weight_dtype,
+__global__ void __launch_bounds__(T, 1) k_add_rmsnorm8(const void* x, size_t x_stride, const void* residual, size_t r_stride, const void* weight, int weight_dtype,
                                                                      float eps, float inv_cols, NormShape n, void* out_sum, size_t s_stride, Held8 out, Held8 kept, float* out_rstd) {
     constexpr int V = vec_elems(DT);
     __shared__ float scratch[32];
@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(T) k_add_rmsnorm8(const void* x, size_t x_stri
 // A CTA takes every gridDim.x-th row (or group of rows); a thread holds the same K vectors of each and adds up its columns' part of the
 // weight's gradient.
 template <int DT, int FMT, int FIT, int K, bool SMALL, int T>
-__global__ void __launch_bounds__(T) k_add_rmsnorm8_backward(const void* dy, size_t dy_stride, const void* dsum, size_t ds_stride, const void* weight,
+__global__ void __launch_bounds__(T, 1) k_add_rmsnorm8_backward(const void* dy, size_t dy_stride, const void* dsum, size_t ds_stride, const void* weight,
                                                                               int weight_dtype, Held8 kept, const float* rstd, float inv_cols, NormShape n, void* dx, size_t dx_stride,
                                                                               float* parts) {
     constexpr int V = vec_elems(DT);
@@ -118,6 +118,18 @@ __global__ void __launch_bounds__(T) k_add_rmsnorm8_backward(const void* dy, siz
     for (size_t first = blockIdx.x * rows_cta; first < n.rows; first += gridDim.x * rows_cta, turn ^= 1) {
         const size_t row = SMALL ? first + threadIdx.x / n.group : first;
         const float rs = row < n.rows ? rstd[row] : 0.0f;
+        // while this row is worked on, L2 fetches the next one
+        if (const size_t after = row + gridDim.x * rows_cta; after < n.rows) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const Place t = place_of<V, SMALL>(n, row, k);
+                if (t.left > 0) {
+                    prefetch_l2(static_cast<const char*>(dy) + (after * dy_stride + t.vec * V) * elem_bytes(DT));
+                    prefetch_l2(kept.codes + after * n.cols + t.vec * V);
+                    if (dsum) prefetch_l2(static_cast<const char*>(dsum) + (after * ds_stride + t.vec * V) * elem_bytes(DT));
+                }
+            }
+        }
         float wd[K][V], xh[K][V];
         float dot = 0.0f;
 #pragma unroll
@@ -303,6 +315,9 @@ __global__ void __launch_bounds__(T, T == 256 ? (RES ? 2 : 3) : T <= 384 ? 2 : 1
 // that is loaded one row ahead has to arrive within that row, because the loop's end moves it (8192 x 4096: 62 us, and 47 like this).
 constexpr int kMeta = 12;   // 32 bytes off the grid lie in 9 words; rstd; 2 unused
 
+// Rows of bf16 beyond 8192 elements take a CTA of 1024 threads, whose 64 registers spill: 4096 x 16384 138 us, half the copy rate.  Two CTAs of 512
+// threads in a cluster, their sums exchanged through shared memory, wait 1.5 us a row for its barriers (129 us, and the norm 124 instead of 97);
+// the weight and dy read again instead of kept cost 15 us more.  The others:
 // 117 registers: two CTAs of up to 320 threads an SM (8192 x 5120 62.5 us with one, 51.4 with two).  Limited to what a third one, or a second
 // one of 384 threads, leaves, the compiler spills (8192 x 4096 41.9 -> 62.4, 8192 x 6144 68.8 -> 88.8).
 template <int DT, int FMT, bool DSUM, int T>
