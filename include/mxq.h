@@ -8,13 +8,15 @@
  *
  * Conventions for every entry point
  *   - Pointers named d_* or documented "device" are DEVICE pointers owned by the caller.  The
- *     library never allocates, frees or keeps them.  All device buffers must be 16-byte aligned.
+ *     library never allocates, frees or keeps them.  All device buffers must be 16-byte aligned
+ *     (those of the 8-bit activations as stated there).
  *   - Calls validate their arguments on the host, enqueue kernels on `cuda_stream` (a
  *     cudaStream_t passed as void*; NULL = the default stream) and return without synchronising.
  *     Nothing is launched when validation fails.
  *   - Return value: MXQ_OK (0) or a positive mxq_status.  Nothing throws, aborts or prints.
  *   - Results are deterministic from run to run (no floating-point atomics).
- *   - Inputs must be finite.  NaN or Inf elements give unspecified (but memory-safe) outputs.
+ *   - Inputs must be finite.  NaN or Inf elements give unspecified (but memory-safe) outputs.  (The calls
+ *     on 8-bit activations say what they make of them.)
  *   - Threads.  Entry points may be called from several host threads at once (on the same or on
  *     different devices and streams): the library keeps no per-call host state, its first-use caches
  *     (SM count, resident CTAs per kernel) are atomics whose racing writers store equal values, and
@@ -317,6 +319,7 @@ int mxq_mask_interval(const void* x, int dtype, size_t n, float lo, float hi, vo
  * De-quantization.  value(code) * S in binary32, then rounded to the output's type.
  * Arithmetic is binary32 unless said otherwise.  rows <= 2^31 - 1, at most 2^41 elements (rows padded to a multiple of
  * 128), MXQ_ERR_TOO_LARGE beyond.  Outputs overlap neither inputs nor one another, except where a call says so.
+ * Aligned pieces of 16 bytes (4 for scale bytes) that hold a byte of an input are read whole.
  */
 typedef enum { MXQ_E4M3 = 0, MXQ_E5M2 = 1 } mxq_elem_fmt;
 

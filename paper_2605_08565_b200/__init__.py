@@ -1,4 +1,4 @@
-"""B200-native block-scaled FP4 quantization, scale search and MSE scoring (libmxq).
+"""B200-native block-scaled FP4 quantization, scale search and MSE scoring, and block-scaled 8-bit activations (libmxq).
 
 ``binding``  ctypes binding of the C-ABI in ``include/mxq.h`` (CUDA only, no fallback)
 ``inputs``   seeded synthetic input generators (no quantization arithmetic)

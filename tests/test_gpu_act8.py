@@ -478,6 +478,35 @@ def test_a_captured_block_replays_with_new_inputs():
         other.check(want_other)
 
 
+def test_four_host_threads_at_once():
+    """Each with its own stream, block and workspace, sixteen steps over: the results of a quiet run."""
+    import threading
+    blocks = [Block(130, 544, 1024, 32, ref.E4M3, 40 + i) for i in range(4)]
+    want = [b.step() for b in blocks]
+    torch.cuda.synchronize()
+    errors = []
+
+    def worker(b, w):
+        try:
+            torch.cuda.set_device(0)
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(16):
+                    got = b.step()
+            torch.cuda.synchronize()
+            for k in ("sum", "y", "dx", "dw"):
+                if not torch.equal(got[k], w[k]):
+                    errors.append(k)
+        except Exception as e:   # a thread's exception would be lost
+            errors.append(repr(e))
+
+    threads = [threading.Thread(target=worker, args=a) for a in zip(blocks, want)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+
+
 def test_a_stream_given_explicitly_is_the_one_that_is_used():
     rows, cols = 64, 4096
     src = torch.randn(rows, cols, device="cuda").to(BF16)
