@@ -478,6 +478,74 @@ def test_a_captured_block_replays_with_new_inputs():
         other.check(want_other)
 
 
+@pytest.mark.parametrize("rows,cols", [(200001, 3), (70000, 16), (9, 4096), (5, 1000)])
+@pytest.mark.parametrize("shift", [0, 1, 2, 3])
+def test_vectors_and_scales_that_start_anywhere(rows, cols, shift):
+    """Scale bytes at any address, weight, rstd, dweight at any element, the workspace at any 16 bytes; many short rows."""
+    B, fmt = 32, ref.E4M3
+    nb = -(-cols // B)
+    x, r, w = norm_inputs(rows, cols, 0, 0, BF16, BF16, 7)
+    w = Guarded(1, cols, BF16, 0, shift).fill(w).view(-1)
+    u8 = lambda n: torch.full((n + 64,), GUARD, dtype=torch.uint8, device="cuda")  # noqa: E731
+    c, kc = u8(rows * cols)[: rows * cols], u8(rows * cols)[: rows * cols]
+    sb, kb = u8(rows * nb), u8(rows * nb)
+    s, ks = sb[shift: shift + rows * nb], kb[shift: shift + rows * nb]
+    total, rstd = torch.empty_like(x), torch.empty(rows + 4, device="cuda")[shift: shift + rows]
+    mxq.mxq_add_rmsnorm8(x, r, w, 1e-5, B, fmt, total, c, s, kc, ks, rstd)
+    h = np64(total)
+    wc, ws = ref.quantize(h, B, fmt)
+    assert np.array_equal(kc.cpu().numpy().reshape(rows, cols), wc) and np.array_equal(ks.cpu().numpy().reshape(rows, nb), ws)
+    for b in (sb, kb):
+        assert bool((b[:shift] == GUARD).all()) and bool((b[shift + rows * nb:] == GUARD).all())
+    y, wr = ref.rmsnorm(h, np64(w), np.float64(np.float32(1e-5)))
+    ref.check_held(c.cpu().numpy().reshape(rows, cols), s.cpu().numpy().reshape(rows, nb), y, rel_of_norm(cols), B, fmt)
+    dy = torch.randn(rows, cols, generator=torch.Generator().manual_seed(3)).to(BF16).cuda()
+    dx, dw = torch.empty_like(dy), torch.full((cols + 8,), -1.0, device="cuda")
+    space = torch.empty(mxq.mxq_add_rmsnorm8_workspace_bytes(rows, cols) // 4 + 16, device="cuda")[4 * shift:]
+    mxq.mxq_add_rmsnorm8_backward(dy, dy, w, kc, ks, rstd, B, fmt, dx, dw[shift: shift + cols], space)
+    wx, ww, size, wsize = ref.rmsnorm_backward(np64(dy), np64(w), ref.dequantize(wc, ws, B, fmt), np64(rstd), np64(dy))
+    assert (np.abs(np64(dx) - wx) <= HALF[BF16] * np.abs(wx) + 65 * U * size).all()
+    assert (np.abs(np64(dw)[shift: shift + cols] - ww) <= (rows + 3) * U * wsize).all()
+    assert bool((dw[:shift] == -1).all()) and bool((dw[shift + cols:] == -1).all())
+    out = torch.empty_like(dx)
+    mxq.mxq_dequantize8(kc, ks, B, fmt, out)
+    assert np.array_equal(np64(out), np64(torch.from_numpy(ref.dequantize(wc, ws, B, fmt)).float().to(BF16)))
+    # the gradient over both of its inputs at once
+    mxq.mxq_add_rmsnorm8_backward(dy, dy, w, kc, ks, rstd, B, fmt, dy)
+    assert torch.equal(dy, dx)
+
+
+def test_first_calls_of_a_process_may_be_captured(tmp_path):
+    """What the first call of a kernel asks of the driver (its limits, how many CTAs fit) may be asked while a stream is captured."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2605_08565_b200 import binding as mxq
+x = torch.randn(700, 2048, device="cuda").to(torch.bfloat16)
+w, rstd = torch.ones(2048, device="cuda"), torch.empty(700, device="cuda")
+h, dx, dw = torch.empty_like(x), torch.empty_like(x), torch.empty(2048, device="cuda")
+q, k, a = (mxq.alloc_outputs8(700, 2048, 32, mxq.MXQ_E4M3, "cuda") for _ in range(3))
+ws = torch.empty(mxq.mxq_add_rmsnorm8_workspace_bytes(700, 2048) // 4, device="cuda")
+def step():
+    mxq.mxq_add_rmsnorm8(x, x, w, 1e-5, 32, mxq.MXQ_E4M3, h, *q, *k, rstd)
+    mxq.mxq_add_rmsnorm8_backward(x, h, w, *k, rstd, 32, mxq.MXQ_E4M3, dx, dw, ws)
+    mxq.mxq_swiglu8(x, h, 32, mxq.MXQ_E4M3, *a)
+    return [t.clone() for t in (h, dx, dw, q[0].view(torch.uint8), a[0].view(torch.uint8))]
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    got = step()
+g.replay()
+torch.cuda.synchronize()
+want = step()
+assert all(torch.equal(a, b) for a, b in zip(got, want))
+print("captured")
+"""
+    r = subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
+
+
 def test_four_host_threads_at_once():
     """Each with its own stream, block and workspace, sixteen steps over: the results of a quiet run."""
     import threading
