@@ -21,7 +21,7 @@ struct Rows8 {
         } else {
             t.row = slot / vectors, t.vec = slot % vectors;
         }
-        t.left = t.row < rows ? (long long)cols - (long long)(t.vec * V) : 0;
+        t.left = t.row < rows ? left_of(cols, t.vec * V) : 0;
         return t;
     }
 };

@@ -138,7 +138,7 @@ __device__ __forceinline__ void store_element(char* to, uint32_t v) {
 // NB bytes to p on, of which the first `valid` are stored, in elements of EB bytes.  A warp's lanes hold consecutive vectors, of one row
 // or of several: `first` tells that a vector starts its row, and `after` counts the bytes that its row holds behind it.  All 32 lanes call it.
 template <int NB, int EB, int FIT>
-__device__ __forceinline__ void store_bytes(void* p, int valid, bool first, long long after, const uint32_t (&w)[NB / 4]) {
+__device__ __forceinline__ void store_bytes(void* p, int valid, bool first, int after, const uint32_t (&w)[NB / 4]) {
     constexpr int N = NB / 4;
     if constexpr (FIT == kWhole) {
         if (valid <= 0) return;
@@ -379,15 +379,19 @@ __device__ __forceinline__ void dequantize_block(const uint32_t* codes, uint32_t
 // One vector: its place in the row and what of the row is left there.
 struct Place {
     size_t row, vec;
-    long long left;   // elements from its first one to the end of the row; <= 0: it lies behind the end
+    int left;   // elements from its first one to the end of the row, a large number for more than that; <= 0: it lies behind the end
 };
+__device__ __forceinline__ int left_of(size_t cols, size_t first) {
+    const long long n = (long long)cols - (long long)first;
+    return n < 1024 ? (int)n : 1024;
+}
 
 // A wide tensor's vector as fp32.
 template <int DT, int FIT, int V>
-__device__ __forceinline__ void load_wide(const void* base, size_t at, long long left, float (&v)[V]) {
+__device__ __forceinline__ void load_wide(const void* base, size_t at, int left, float (&v)[V]) {
     constexpr int EB = elem_bytes(DT);
     uint32_t w[V * EB / 4];
-    load_bytes<V * EB, EB, FIT>(static_cast<const char*>(base) + at * EB, left >= V ? V * EB : (int)left * EB, w);
+    load_bytes<V * EB, EB, FIT>(static_cast<const char*>(base) + at * EB, min(left, V) * EB, w);
     unpack<DT, V>(w, v);
 }
 template <int DT, int FIT, int V>
@@ -395,7 +399,7 @@ __device__ __forceinline__ void store_wide(void* base, size_t at, const Place& t
     constexpr int EB = elem_bytes(DT);
     uint32_t w[V * EB / 4];
     pack<DT, V>(v, w);
-    store_bytes<V * EB, EB, FIT>(static_cast<char*>(base) + at * EB, t.left >= V ? V * EB : (int)t.left * EB, t.vec == 0, (t.left - V) * EB, w);
+    store_bytes<V * EB, EB, FIT>(static_cast<char*>(base) + at * EB, min(t.left, V) * EB, t.vec == 0, (t.left - V) * EB, w);
 }
 
 // Quantizes and stores this thread's vector; the first lane of a block stores the scale.  The whole warp calls it.
@@ -403,14 +407,14 @@ template <int FMT, int FIT, int V>
 __device__ __forceinline__ void put_held(const Held8& out, const float (&v)[V], const Place& t, size_t cols, size_t blocks, int lanes_log2) {
     uint32_t c[V / 4];
     const uint32_t byte = quantize_block<FMT, V>(v, lanes_log2, c);
-    store_bytes<V, 1, FIT>(out.codes + t.row * cols + t.vec * V, t.left >= V ? V : (int)t.left, t.vec == 0, t.left - V, c);
+    store_bytes<V, 1, FIT>(out.codes + t.row * cols + t.vec * V, min(t.left, V), t.vec == 0, t.left - V, c);
     if (t.left > 0 && (t.vec & (size_t)((1 << lanes_log2) - 1)) == 0) out.scales[t.row * blocks + (t.vec >> lanes_log2)] = (uint8_t)byte;
 }
 
 template <int FMT, int FIT, int V>
 __device__ __forceinline__ void get_held(const Held8& in, float (&v)[V], const Place& t, size_t cols, size_t blocks, int lanes_log2) {
     uint32_t c[V / 4];
-    load_bytes<V, 1, FIT>(in.codes + t.row * cols + t.vec * V, t.left >= V ? V : (int)t.left, c);
+    load_bytes<V, 1, FIT>(in.codes + t.row * cols + t.vec * V, min(t.left, V), c);
     const uint32_t byte = t.left > 0 ? in.scales[t.row * blocks + (t.vec >> lanes_log2)] : 0u;
     dequantize_block<FMT, V>(c, byte, v);
 }
