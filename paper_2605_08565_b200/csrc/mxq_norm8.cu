@@ -4,7 +4,6 @@
 
 #include "mxq_act8.cuh"
 
-
 namespace mxq {
 
 // How rows are laid over threads.
@@ -313,9 +312,6 @@ __global__ void __launch_bounds__(T, T == 256 ? (RES ? 2 : 3) : T <= 384 ? 2 : 1
 // that is loaded one row ahead has to arrive within that row, because the loop's end moves it (8192 x 4096: 62 us, and 47 like this).
 constexpr int kMeta = 12;   // 32 bytes off the grid lie in 9 words; rstd; 2 unused
 
-// Rows of bf16 beyond 8192 elements take a CTA of 1024 threads, whose 64 registers spill: 4096 x 16384 138 us, half the copy rate.  Two CTAs of 512
-// threads in a cluster, their sums exchanged through shared memory, wait 1.5 us a row for its barriers (129 us, and the norm 124 instead of 97);
-// the weight and dy read again instead of kept cost 15 us more.  The others:
 // 117 registers: two CTAs of up to 320 threads an SM (8192 x 5120 62.5 us with one, 51.4 with two).  Limited to what a third one, or a second
 // one of 384 threads, leaves, the compiler spills (8192 x 4096 41.9 -> 62.4, 8192 x 6144 68.8 -> 88.8).
 template <int DT, int FMT, bool DSUM, int T>
@@ -422,6 +418,125 @@ __global__ void __launch_bounds__(T, T <= 320 ? 2 : 1)
 #pragma unroll
         for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(dw[j + i]);
         store256(parts + blockIdx.x * n.cols + t.vec * V + j, b);
+    }
+}
+
+// The same for rows of 8193 to 16384 bf16 elements: 512 threads of two vectors.  Nothing but the weight's gradient is kept in registers; dy and the codes
+// are read from the copy and the weight from L1 before the barrier and again behind it.  4096 x 16384: 118 us, and 138 with a CTA of 1024 threads, whose 64
+// registers spill; two CTAs of 512 threads in a cluster, their sums exchanged through shared memory, wait 1.5 us a row for its barriers (129 us).
+template <int FMT, bool DSUM>
+__global__ void __launch_bounds__(512, 1)
+    k_add_rmsnorm8_backward_wide(const char* dy, size_t dy_step, const char* dsum, size_t ds_step, const void* weight, int weight_dtype, Held8 kept, const float* rstd,
+                                 float inv_cols, NormShape n, char* dx, size_t dx_step, float* parts) {
+    constexpr int V = 16, K = 2, T = 512, C = DSUM ? 5 : 3;
+    const int n_thr = blockDim.x, half = C * n_thr + kMeta * n_thr / 128, slot_size = K * half;   // half: one vector a thread
+    extern __shared__ uint4 ring[];
+    __shared__ float4 sums[2][T / 128];
+    wait_for_prior_grid();
+    release_dependents();
+    const int lane = threadIdx.x & 31, warp0 = threadIdx.x & ~31;
+    const size_t step = gridDim.x;
+    size_t row = blockIdx.x;
+    auto fetch = [&](uint4* to, size_t r) {
+#pragma unroll
+        for (int k = 0; k < K; ++k, to += half) {
+            const size_t vec0 = (size_t)k * n_thr + warp0;   // the warp's first vector
+            const WarpCopy copy(((long long)n.cols - (long long)vec0 * V) * 2);
+            copy(to + warp0 * 2, dy + r * dy_step + vec0 * 32 + lane * 16);
+            if constexpr (DSUM) copy(to + 2 * n_thr + warp0 * 2, dsum + r * ds_step + vec0 * 32 + lane * 16);
+            if ((vec0 + lane) * V < n.cols) copy_async16(to + (C - 1) * n_thr + threadIdx.x, kept.codes + r * n.cols + (vec0 + lane) * V);
+            const size_t block0 = vec0 >> n.lanes_log2;
+            const int bytes = (int)min((long long)(32 >> n.lanes_log2), (long long)n.blocks - (long long)block0);
+            const uint8_t* const pb = kept.scales + r * n.blocks + block0;
+            const int off = (int)(reinterpret_cast<uintptr_t>(pb) & 3u);
+            uint32_t* const meta = reinterpret_cast<uint32_t*>(to + C * n_thr) + kMeta * (threadIdx.x / 32);
+            if (lane < 9 ? bytes > 0 && 4 * lane < off + bytes : lane == 9) copy_async4(meta + lane, lane < 9 ? (const void*)(pb - off + 4 * lane) : (const void*)(rstd + r));
+        }
+    };
+    // dy and n = h rstd of this thread's k-th vector of the row in `slot`
+    auto read = [&](const uint4* slot, int k, const Place& t, float (&d)[V], float (&xh)[V]) {
+        const uint4* const at = slot + k * half;
+        const uint32_t* const meta = reinterpret_cast<const uint32_t*>(at + C * n_thr) + kMeta * (threadIdx.x / 32);
+        uint32_t a[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u}, c[V / 4] = {}, byte = 0u;
+        const float rs = __uint_as_float(meta[9]);
+        if (t.left > 0) {
+            read32(at + warp0 * 2, a);
+            const uint4 q = at[(C - 1) * n_thr + threadIdx.x];
+            c[0] = q.x, c[1] = q.y, c[2] = q.z, c[3] = q.w;
+            const size_t first = row * n.blocks + (((size_t)k * n_thr + warp0) >> n.lanes_log2);
+            byte = reinterpret_cast<const uint8_t*>(meta)[((unsigned)reinterpret_cast<uintptr_t>(kept.scales + first) & 3u) + (lane >> n.lanes_log2)];
+        }
+        unpack<kBF16, V>(a, d);
+        dequantize_block<FMT, V>(c, byte, xh);
+#pragma unroll
+        for (int j = 0; j < V; j += 2) {
+            const float2 h = mul2(make_float2(xh[j], xh[j + 1]), make_float2(rs, rs));
+            xh[j] = h.x, xh[j + 1] = h.y;
+        }
+        return rs;
+    };
+    if (threadIdx.x < sizeof(sums) / 4) reinterpret_cast<float*>(sums)[threadIdx.x] = 0.0f;
+    uint4* slot = ring;
+    uint4* other = ring + slot_size;
+    fetch(slot, row);
+    copy_commit();
+    float dw[K][V];
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int j = 0; j < V; ++j) dw[k][j] = 0.0f;
+    __syncthreads();   // the zeros in `sums`
+    for (int turn = 0; row < n.rows; row += step, turn ^= 1) {
+        __syncwarp();   // the other lanes have read what the next copies replace
+        if (row + step < n.rows) fetch(other, row + step);
+        copy_commit();
+        copy_wait<1>();
+        __syncwarp();
+        float2 dot = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const Place t = place_of<V, false>(n, row, k);
+            float d[V], xh[V], w[V];
+            load_weight<kWhole, V>(weight, weight_dtype, t, w);
+            read(slot, k, t, d, xh);
+#pragma unroll
+            for (int j = 0; j < V; j += 2) {
+                const float2 y = make_float2(d[j], d[j + 1]), h = make_float2(xh[j], xh[j + 1]);
+                const float2 s = fma2(y, h, make_float2(dw[k][j], dw[k][j + 1]));
+                dot = fma2(mul2(y, make_float2(w[j], w[j + 1])), h, dot);
+                dw[k][j] = s.x, dw[k][j + 1] = s.y;
+            }
+        }
+        const float c = -cta_sum<T>(dot.x + dot.y, reinterpret_cast<float*>(sums[turn])) * inv_cols;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const Place t = place_of<V, false>(n, row, k);
+            float d[V], xh[V], w[V], ds[V];
+            load_weight<kWhole, V>(weight, weight_dtype, t, w);
+            const float rs = read(slot, k, t, d, xh);
+            uint32_t b[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+            if constexpr (DSUM)
+                if (t.left > 0) read32(slot + k * half + 2 * n_thr + warp0 * 2, b);
+            unpack<kBF16, V>(b, ds);
+#pragma unroll
+            for (int j = 0; j < V; j += 2) {
+                float2 e = fma2(make_float2(xh[j], xh[j + 1]), make_float2(c, c), mul2(make_float2(d[j], d[j + 1]), make_float2(w[j], w[j + 1])));
+                if constexpr (DSUM) e = fma2(e, make_float2(rs, rs), make_float2(ds[j], ds[j + 1]));
+                else e = mul2(e, make_float2(rs, rs));
+                ds[j] = e.x, ds[j + 1] = e.y;
+            }
+            pack<kBF16, V>(ds, b);
+            if (t.left > 0) store256(dx + row * dx_step + t.vec * 32, b);
+        }
+        uint4* const done = slot;
+        slot = other;
+        other = done;
+    }
+    if (!parts) return;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const Place t = place_of<V, false>(n, 0, k);
+        store_wide<kF32, kWhole>(parts, blockIdx.x * n.cols + t.vec * V, t, dw[k]);
     }
 }
 
@@ -591,15 +706,20 @@ cudaError_t launch_add_rmsnorm8_backward(const Wide8& dy, const Wide8& dsum, con
         err = pick_rows(dtype, fmt, l, [&](auto dt, auto fm, auto threads) {
             auto go = [&](auto ds) {
                 static std::atomic<int> cache[33][kMaxDevices];
-                auto* kernel = k_add_rmsnorm8_backward_rows<dt(), fm(), ds(), threads()>;
+                auto launch = [&](auto* kernel, unsigned n, auto smem_of, unsigned most) {
+                    cudaError_t e = rows_grid((const void*)kernel, smem_of(n), smem_of(most), n, cache, rows, kNorm8Parts, grid);
+                    if (e != cudaSuccess) return e;
+                    count_launch();
+                    const size_t es = dtype == kF32 ? 4 : 2;
+                    return launch_pdl(kernel, grid, n, smem_of(n), s, (const char*)dy.p, dy.stride * es, (const char*)dsum.p, dsum.stride * es, weight, weight_dtype, kept, rstd,
+                                      1.0f / (float)cols, l.n, (char*)dx.p, dx.stride * es, dweight ? parts : (float*)nullptr);
+                };
                 auto smem_of = [&](size_t n) { return 2 * ((ds() ? 5 : 3) * n * 16 + kMeta * n / 8); };
-                const size_t smem = smem_of(l.threads);
-                cudaError_t e = rows_grid((const void*)kernel, smem, smem_of(threads()), l.threads, cache, rows, kNorm8Parts, grid);
-                if (e != cudaSuccess) return e;
-                count_launch();
-                const size_t es = dtype == kF32 ? 4 : 2;
-                return launch_pdl(kernel, grid, l.threads, smem, s, (const char*)dy.p, dy.stride * es, (const char*)dsum.p, dsum.stride * es, weight, weight_dtype, kept, rstd,
-                                  1.0f / (float)cols, l.n, (char*)dx.p, dx.stride * es, dweight ? parts : (float*)nullptr);
+                if constexpr (dt() == kBF16 && threads() == 1024) {
+                    return launch(k_add_rmsnorm8_backward_wide<fm(), ds()>, (l.threads / 2 + 31) / 32 * 32, [&](size_t n) { return 2 * smem_of(n); }, 512u);
+                } else {
+                    return launch(k_add_rmsnorm8_backward_rows<dt(), fm(), ds(), threads()>, l.threads, smem_of, (unsigned)threads());
+                }
             };
             return dsum.p ? go(std::integral_constant<bool, true>{}) : go(std::integral_constant<bool, false>{});
         });
