@@ -223,11 +223,12 @@ __device__ __forceinline__ void read32(const uint4* from, uint32_t (&w)[8]) {
     w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
 }
 
-// Two CTAs of 256 threads an SM and the registers that they leave are faster than three with fewer (8192 x 4096, us: with the residual and
-// the checkpoint 43.5 / 49.1, with the residual 37.7 / 39.9) and slower without a residual (with the checkpoint 27.9 / 24.7).  CTAs of 320 and
-// 384 threads would else be alone on their SM.
+// Resident CTAs.  With a residual two of 256 threads and the registers that they leave are faster than three with fewer (8192 x 4096, us: with the
+// checkpoint too 43.5 / 49.1, else 37.7 / 39.9), two of 384 than one, one of 512 or 1024 is enough.  Without, half as much is under way from memory for each,
+// and more of them are better: four of 256 (three: 20.1 -> 19.2, with the checkpoint 24.7 -> 23.8), three of 384 (8192 x 5120 26.5 -> 24.2), two of
+// 512 (8192 x 8192 47.0 -> 37.6).
 template <int DT, int FMT, bool RES, bool KEEP, int T>
-__global__ void __launch_bounds__(T, T == 256 ? (RES ? 2 : 3) : T <= 384 ? 2 : 1)
+__global__ void __launch_bounds__(T, T == 256 ? (RES ? 2 : 4) : T <= 384 ? (RES ? 2 : 3) : T == 512 && !RES ? 2 : 1)
     k_add_rmsnorm8_rows(const char* x, size_t x_step, const char* residual, size_t r_step, const void* weight, int weight_dtype, float eps, float inv_cols, NormShape n,
                         char* out_sum, size_t s_step, Held8 out, Held8 kept, float* out_rstd) {
     constexpr int V = vec_elems(DT);
