@@ -307,7 +307,8 @@ static int check8(size_t rows, size_t cols, int dtype, int block_size, int elem_
     if (dtype != MXQ_F32 && dtype != MXQ_BF16) return MXQ_ERR_BAD_ENUM;
     if (elem_fmt != MXQ_E4M3 && elem_fmt != MXQ_E5M2) return MXQ_ERR_BAD_ENUM;
     if (!valid_block8(block_size) || rows == 0 || cols == 0) return MXQ_ERR_BAD_SHAPE;
-    if (rows > kAct8MaxRows || cols > kAct8MaxElems || rows * ((cols + 127) / 128 * 128) > kAct8MaxElems) return MXQ_ERR_TOO_LARGE;
+    if (rows > kAct8MaxRows || cols > kAct8MaxElems) return MXQ_ERR_TOO_LARGE;
+    if ((cols + 127) / 128 * 128 > kAct8MaxElems / rows) return MXQ_ERR_TOO_LARGE;   // not by the product, which may pass 2^64
     return MXQ_OK;
 }
 // A tensor whose rows lie `stride` elements apart.

@@ -75,6 +75,18 @@ def test_swiglu8_refuses(lib):
               (dict(su=60), 3), (dict(dgate=G), 3), (dict(dgate=A, sg=72), 3), (dict(dup=A, su=72), 3), (dict(dup=G + 2), 4)])
 
 
+@pytest.mark.parametrize("rows,cols", [(1 << 30, 1 << 34), (1 << 30, (1 << 34) + 128), (1 << 27, 1 << 37), ((1 << 31) - 1, 1 << 33), (1 << 24, 1 << 41), (1 << 15, (1 << 26) + 1)])
+def test_sizes_whose_product_passes_64_bits_are_too_large(lib, rows, cols):
+    """Four products of rows and padded cols are small modulo 2^64, one comes close to it, and the last one is past the limit by its padding alone."""
+    assert rows * -(-cols // 128) * 128 > 1 << 41
+    assert lib.mxq_quantize8(A, 0, rows, cols, cols, 32, 0, B_, C, 0) == 8
+    assert lib.mxq_dequantize8(A, B_, rows, cols, 32, 0, C, 0, cols, 0) == 8
+    assert lib.mxq_swiglu8(A, B_, 0, rows, cols, cols, cols, 32, 0, C, D, 0, 0, 0, 0, 0) == 8
+    assert lib.mxq_swiglu8_backward(A, 0, rows, cols, cols, B_, C, D, E, 32, 0, F, cols, G, cols, 0) == 8
+    assert lib.mxq_add_rmsnorm8(A, 0, C, 0, 0, rows, cols, cols, 0, 1e-5, 32, 0, 0, 0, E, F, 0, 0, 0, 0) == 8
+    assert lib.mxq_add_rmsnorm8_backward(A, 0, C, 0, 0, rows, cols, cols, 0, D, E, F, 32, 0, G, cols, 0, 0, 0, 0) == 8
+
+
 def test_binding_refuses_what_is_not_on_a_gpu(lib):
     from paper_2605_08565_b200 import binding as mxq
     x, c, s = torch.zeros(4, 64), torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(4, 2, dtype=torch.uint8)
