@@ -360,7 +360,9 @@ int mxq_add_rmsnorm8(const void* x, const void* residual, const void* weight, in
  *   dweight  cols floats, overwritten, or NULL: not wanted.
  *   d_workspace  needed for dweight: mxq_add_rmsnorm8_workspace_bytes(rows, cols) bytes, 16-byte aligned; overwritten, need
  *            not be cleared.  Calls that may run at the same time need one each.
- * The rows are added up in an order that depends on rows, cols and the device alone: the same inputs give the same bits.
+ * Sums are formed in a fixed order, without atomics: calls that are alike in shape, types, block_size, strides, the tensors given (dsum or not)
+ * and the device give the same bits, as long as the rows of dy, dsum and dx and the weight start alike modulo 32 bytes (kernels are chosen by that).
+ * The workspace's address, and whether dweight is asked for, change no bit of dx.
  */
 size_t mxq_add_rmsnorm8_workspace_bytes(size_t rows, size_t cols);
 int mxq_add_rmsnorm8_backward(const void* dy, const void* dsum, const void* weight, int dtype, int weight_dtype,

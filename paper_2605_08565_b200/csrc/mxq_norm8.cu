@@ -104,7 +104,8 @@ __global__ void __launch_bounds__(T, T == 512 ? 3 : 1) k_add_rmsnorm8(const void
 }
 
 // A CTA takes every gridDim.x-th row (or group of rows); a thread holds the same K vectors of each and adds up its columns' part of the
-// weight's gradient.
+// weight's gradient.  The parts (here and in the kernels below) are stored 16 bytes at a time, which every workspace allows: its address has no say
+// in which kernel runs, so that dx and dweight are the same bits with any workspace.
 // Registers for two CTAs of 512 threads an SM: 8192 x 4101 bf16 146 us with one, 100 with two (8192 x 4104: 101, 58); limiting those of 256 threads to
 // three an SM costs 0 to 20 %.
 template <int DT, int FMT, int FIT, int K, bool SMALL, int T>
@@ -191,7 +192,7 @@ __global__ void __launch_bounds__(T, T == 512 ? 2 : 1) k_add_rmsnorm8_backward(c
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const Place t = place_of<V, SMALL>(n, 0, k);
-            store_wide<kF32, FIT>(parts, blockIdx.x * n.cols + t.vec * V, t, dw[k]);
+            store_wide<kF32, FIT == kAny ? kAny : kHalf>(parts, blockIdx.x * n.cols + t.vec * V, t, dw[k]);
         }
     }
 }
@@ -412,14 +413,7 @@ __global__ void __launch_bounds__(T, T <= 320 ? 2 : 1)
         slot = other;
         other = done;
     }
-    if (!parts || !here) return;
-#pragma unroll
-    for (int j = 0; j < V; j += 8) {
-        uint32_t b[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(dw[j + i]);
-        store256(parts + blockIdx.x * n.cols + t.vec * V + j, b);
-    }
+    if (parts) store_wide<kF32, kHalf>(parts, blockIdx.x * n.cols + t.vec * V, t, dw);
 }
 
 // The same for rows of 8193 to 16384 bf16 elements: 512 threads of two vectors.  Nothing but the weight's gradient is kept in registers; dy and the codes
@@ -537,7 +531,7 @@ __global__ void __launch_bounds__(512, 1)
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const Place t = place_of<V, false>(n, 0, k);
-        store_wide<kF32, kWhole>(parts, blockIdx.x * n.cols + t.vec * V, t, dw[k]);
+        store_wide<kF32, kHalf>(parts, blockIdx.x * n.cols + t.vec * V, t, dw[k]);
     }
 }
 
@@ -700,7 +694,6 @@ cudaError_t launch_add_rmsnorm8_backward(const Wide8& dy, const Wide8& dsum, con
     const NormLaunch l = norm_launch(rows, cols, B, dtype);
     int fit = worst_fit(worst_fit(fit_of(dy, cols, dtype), fit_of(dx, cols, dtype)), fit_of_weight(weight, weight_dtype, dtype, cols));
     if (dsum.p) fit = worst_fit(fit, fit_of(dsum, cols, dtype));
-    if (dweight) fit = worst_fit(fit, fit_of_weight(parts, kF32, dtype, cols));
     unsigned grid = 0;
     cudaError_t err;
     if (rows_fit(l, fit)) {

@@ -616,3 +616,24 @@ def test_offsets_past_32_bits():
     mxq.mxq_dequantize8(c, s, 32, ref.E4M3, x)
     assert np.array_equal(np64(x), ref.dequantize(wc, ws, 32, ref.E4M3).astype(np.float32).astype(np.float64)) or \
         torch.equal(x.cpu(), torch.from_numpy(ref.dequantize(wc, ws, 32, ref.E4M3)).float().to(BF16))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("cols,pad,shift", [(1024, 0, 0), (4096, 0, 0), (8192, 0, 0), (16384, 0, 0), (32768, 0, 0), (4104, 0, 0), (1000, 3, 1), (128, 0, 0)])
+def test_the_workspace_changes_no_bit_of_the_gradients(cols, pad, shift, dtype):
+    """On 32, 16 bytes, or not there: the kernels of whole, halved and shifted rows, one row of each and several."""
+    rows = 400
+    dy, ds, w, codes, scales, rstd = backward_inputs(rows, cols, pad, shift, dtype, F32, ref.E4M3, 32, cols)
+    got = []
+    for at in (None, 0, 4, 12):
+        dx, dw = Guarded(rows, cols, dtype, pad, shift), Guarded(1, cols, F32)
+        room = mxq.mxq_add_rmsnorm8_workspace_bytes(rows, cols) // 4
+        ws = Guarded(1, room, F32, 0, at or 0)
+        if at is None:
+            mxq.mxq_add_rmsnorm8_backward(dy, ds, w, codes, scales, rstd, 32, ref.E4M3, dx.t)
+        else:
+            mxq.mxq_add_rmsnorm8_backward(dy, ds, w, codes, scales, rstd, 32, ref.E4M3, dx.t, dw.t, ws.t.view(-1))
+        assert dx.untouched() and dw.untouched() and ws.untouched()
+        got.append((dx.t, dw.t))
+    for dx, dw in got[1:]:
+        assert torch.equal(dx, got[0][0]) and torch.equal(dw, got[1][1])
