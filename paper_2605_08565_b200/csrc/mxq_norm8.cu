@@ -596,8 +596,11 @@ static cudaError_t pick(int dtype, int fmt, int fit, const NormLaunch& l, F f) {
             if (l.K == 1 && l.threads <= 512) return f(dt, fm, fit, integral_constant<int, 1>{}, No{}, integral_constant<int, 512>{});
             if (l.K == 1) return f(dt, fm, fit, integral_constant<int, 1>{}, No{}, integral_constant<int, 1024>{});
         }
-        return l.K == 2 ? f(dt, fm, fit, integral_constant<int, 2>{}, No{}, integral_constant<int, 1024>{})
-                        : f(dt, fm, fit, integral_constant<int, 4>{}, No{}, integral_constant<int, 1024>{});
+        static_assert(kNorm8MaxCols <= 2 * 1024 * vec_elems(kBF16) && kNorm8MaxCols <= 4 * 1024 * vec_elems(kF32), "vectors of a thread");
+        if constexpr (dt() == kF32) {
+            if (l.K == 4) return f(dt, fm, fit, integral_constant<int, 4>{}, No{}, integral_constant<int, 1024>{});
+        }
+        return f(dt, fm, fit, integral_constant<int, 2>{}, No{}, integral_constant<int, 1024>{});
     };
     auto by_fit = [&](auto dt, auto fm) {
         return fit == kWhole  ? by_k(dt, fm, integral_constant<int, kWhole>{})
