@@ -637,3 +637,58 @@ def test_the_workspace_changes_no_bit_of_the_gradients(cols, pad, shift, dtype):
         got.append((dx.t, dw.t))
     for dx, dw in got[1:]:
         assert torch.equal(dx, got[0][0]) and torch.equal(dw, got[1][1])
+
+
+def dequantize64(codes, scales, B, fmt):
+    """The values of 8-bit codes (bytes), in binary64 on the device."""
+    table = torch.from_numpy(ref.value_of(np.arange(256, dtype=np.uint8), fmt)).cuda()
+    s = torch.exp2(scales.double() - 127).repeat_interleave(B, 1)[:, : codes.shape[1]]
+    return table[codes.long()] * s
+
+
+# Every kernel of the gradient with more rows (or groups of rows) than it has CTAs: rows that share a warp; whole, halved and shifted rows of CTAs of
+# 256, 512 and 1024 threads; the streaming kernels; two and four vectors a thread.
+MANY_ROWS = [(F32, 200001, 3, 0, 0), (BF16, 200001, 3, 0, 0), (BF16, 70000, 16, 0, 0), (BF16, 90001, 24, 0, 0), (F32, 40000, 200, 0, 0), (BF16, 30000, 500, 1, 1),
+             (F32, 1500, 1001, 1, 1), (BF16, 1500, 1001, 0, 0), (BF16, 1500, 1000, 8, 0), (F32, 900, 2501, 0, 0), (BF16, 900, 5001, 0, 1), (BF16, 900, 4104, 0, 0),
+             (F32, 400, 5001, 0, 0), (BF16, 400, 9001, 3, 0), (BF16, 400, 8200, 0, 0), (F32, 400, 9001, 0, 0), (BF16, 400, 16389, 0, 0), (BF16, 400, 20008, 0, 0),
+             (BF16, 400, 32768, 0, 0), (F32, 400, 17001, 0, 1), (F32, 400, 20004, 0, 0), (F32, 400, 32768, 0, 0), (F32, 400, 16384, 0, 0), (BF16, 900, 1024, 0, 0),
+             (BF16, 900, 5120, 0, 0), (BF16, 900, 6144, 0, 0), (BF16, 900, 8192, 0, 0), (BF16, 400, 16384, 0, 0), (F32, 900, 2048, 0, 0), (F32, 900, 8192, 0, 0)]
+
+
+@pytest.mark.parametrize("with_dsum", [True, False])
+@pytest.mark.parametrize("dtype,rows,cols,pad,shift", MANY_ROWS)
+def test_gradient_of_the_weight_counts_every_row(dtype, rows, cols, pad, shift, with_dsum):
+    """dy has the sign of h, so that every row adds to dweight, and the bound counts the additions that are made: what a CTA takes in one turn is far above it."""
+    B, fmt = 16, ref.E4M3
+    g = torch.Generator(device="cuda").manual_seed(rows + cols)
+    rand = lambda *n: torch.randn(*n, generator=g, device="cuda")  # noqa: E731
+    codes, scales = (t.view(torch.uint8) for t in mxq.quantize8(rand(rows, cols), B, fmt))
+    h = dequantize64(codes, scales, B, fmt)
+    rstd = (h.square().mean(1) + 1e-5).rsqrt().float()
+    dy = Guarded(rows, cols, dtype, pad, shift).fill((1 + rand(rows, cols).abs()) * torch.where(h < 0, -1.0, 1.0).float())
+    ds = Guarded(rows, cols, dtype, pad, shift).fill(rand(rows, cols)) if with_dsum else None
+    w = 1 + 0.2 * rand(cols)
+    dx, dw = Guarded(rows, cols, dtype, pad, shift), Guarded(1, cols, F32)
+    mxq.mxq_add_rmsnorm8_backward(dy, ds, w, codes, scales, rstd, B, fmt, dx.t, dw.t, workspace(rows, cols))
+    assert dx.untouched() and dw.untouched()
+    r, n = rstd.double()[:, None], h * rstd.double()[:, None]
+    wd = w.double() * dy.double()
+    mean, size_of_mean = (wd * n).mean(1, keepdim=True), (wd * n).abs().mean(1, keepdim=True)
+    want, size = r * (wd - n * mean), r * (wd.abs() + n.abs() * size_of_mean)
+    if with_dsum:
+        want, size = want + ds.double(), size + ds.double().abs()
+    assert bool(((dx.t.double() - want).abs() <= HALF[dtype] * want.abs() + 65 * U * size).all())    # as in test_add_rmsnorm8_backward
+    # dweight: the rounding of n; a turn each of a thread, of which a CTA has the fewer the more CTAs there are (one an SM at least); the groups of
+    # rows of a CTA, one after the other; at most 1024 parts, every 32nd by a warp, and a tree over the warps
+    vectors = -(-cols // B) * (B // (8 if dtype == F32 else 16))
+    group = 1 << max(0, (vectors - 1).bit_length()) if vectors <= 32 else 0
+    rows_cta = 256 // group if group else 1
+    work = -(-rows // rows_cta)
+    turns = -(-work // min(work, torch.cuda.get_device_properties(0).multi_processor_count))
+    terms = dy.double() * n
+    total = terms.sum(0)
+    bound = (1 + turns + (rows_cta if group else 0) + min(work, 1024) // 32 + 1 + 5) * U * terms.abs().sum(0)
+    assert bool(((dw.t[0].double() - total).abs() <= bound).all())
+    # without what one CTA adds in one turn the check would fail, whichever turn it is
+    parts = torch.nn.functional.pad(terms, (0, 0, 0, work * rows_cta - rows)).view(work, rows_cta, cols).sum(1)
+    assert bool((parts.abs() > 2 * bound).any(1).all())
