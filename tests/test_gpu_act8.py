@@ -692,3 +692,61 @@ def test_gradient_of_the_weight_counts_every_row(dtype, rows, cols, pad, shift, 
     # without what one CTA adds in one turn the check would fail, whichever turn it is
     parts = torch.nn.functional.pad(terms, (0, 0, 0, work * rows_cta - rows)).view(work, rows_cta, cols).sum(1)
     assert bool((parts.abs() > 2 * bound).any(1).all())
+
+
+@pytest.mark.parametrize("dtype,rows,cols,pad,shift", [(BF16, 9, 1001, 3, 1), (F32, 9, 1001, 0, 1), (BF16, 40, 2501, 0, 0), (F32, 40, 2502, 0, 2), (BF16, 7, 8193, 0, 3), (F32, 5, 8190, 0, 0),
+                                                       (BF16, 3, 20001, 1, 0), (F32, 3, 20001, 0, 0), (BF16, 300, 77, 0, 0), (BF16, 6, 4104, 0, 0)])
+def test_norm_and_gradient_in_place_on_shifted_rows(dtype, rows, cols, pad, shift):
+    """Over either summand, over dy and over dsum, where neighbouring rows, warps and vectors of a thread share 16-byte pieces."""
+    x, r, w = norm_inputs(rows, cols, pad, shift, dtype, F32, cols)
+    got = []
+    for over in (None, "x", "residual"):
+        a, b = Guarded(rows, cols, dtype, pad, shift), Guarded(rows, cols, dtype, pad, shift)
+        a.fill(x), b.fill(r)
+        out = {None: Guarded(rows, cols, dtype, pad, shift), "x": a, "residual": b}[over]
+        held, kept, rstd = held_out(rows, cols, 16), held_out(rows, cols, 16), torch.empty(rows, device="cuda")
+        mxq.mxq_add_rmsnorm8(a.t, b.t, w, 1e-5, 16, ref.E4M3, out.t, held[0].t, held[1].t, kept[0].t, kept[1].t, rstd)
+        assert out.untouched() and all(t.untouched() for t in held + kept)
+        got.append([out.t, rstd] + [t.t for t in held + kept])
+    assert torch.equal(got[0][0], (x.float() + r.float()).to(dtype))
+    for other in got[1:]:
+        assert all(torch.equal(p, q) for p, q in zip(other, got[0]))
+    rstd, kept = got[0][1], [got[0][4].view(rows, cols), got[0][5].view(rows, -1)]
+    got = []
+    for over in (None, "dy", "dsum", "both"):
+        a, b = Guarded(rows, cols, dtype, pad, shift), Guarded(rows, cols, dtype, pad, shift)
+        a.fill(x), b.fill(x if over == "both" else r)
+        out = {None: Guarded(rows, cols, dtype, pad, shift), "dy": a, "dsum": b, "both": a}[over]
+        dw = torch.empty(cols, device="cuda")
+        mxq.mxq_add_rmsnorm8_backward(a.t, a.t if over == "both" else b.t, w, *kept, rstd, 16, ref.E4M3, out.t, dw, workspace(rows, cols))
+        assert out.untouched()
+        if over == "both":
+            plain = Guarded(rows, cols, dtype, pad, shift)
+            mxq.mxq_add_rmsnorm8_backward(b.t, b.t, w, *kept, rstd, 16, ref.E4M3, plain.t)
+            assert torch.equal(out.t, plain.t)
+        else:
+            got.append((out.t, dw))
+    for dx, dw in got[1:]:
+        assert torch.equal(dx, got[0][0]) and torch.equal(dw, got[0][1])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,cols,B", [(33, 256, 32), (5, 4096, 16), (3, 9216, 128), (2, 20480, 64)])
+def test_where_rows_start_changes_no_bit_that_is_elementwise(rows, cols, B, dtype):
+    """Whole, halved and shifted rows of the same values: sums, codes of given tensors, the gated activation and its gradient are the same bits."""
+    x, r, w = norm_inputs(rows, cols, 0, 0, dtype, F32, cols)
+    first = None
+    for pad, shift in ((0, 0), (0, 16 // x.element_size()), (3, 1), (8, 5)):
+        put = lambda v: Guarded(rows, cols, dtype, pad, shift).fill(v)  # noqa: E731
+        a, b = put(x), put(r)
+        wide = [Guarded(rows, cols, dtype, pad, shift) for _ in range(4)]
+        y, kept, q, act, gk, uk = (held_out(rows, cols, B) for _ in range(6))
+        mxq.mxq_add_rmsnorm8(a, b, w, 1e-5, B, ref.E4M3, wide[0].t, y[0].t, y[1].t, kept[0].t, kept[1].t)
+        mxq.mxq_quantize8(a, B, ref.E4M3, q[0].t, q[1].t)
+        mxq.mxq_dequantize8(q[0].t, q[1].t, B, ref.E4M3, wide[1].t)
+        mxq.mxq_swiglu8(a, b, B, ref.E4M3, act[0].t, act[1].t, gk[0].t, gk[1].t, uk[0].t, uk[1].t)
+        mxq.mxq_swiglu8_backward(b, gk[0].t, gk[1].t, uk[0].t, uk[1].t, B, ref.E4M3, wide[2].t, wide[3].t)
+        assert all(t.untouched() for t in wide)
+        out = [t.t.clone() for t in wide] + [t.t.clone() for pair in (kept, q, act, gk, uk) for t in pair]
+        first = first or out
+        assert all(torch.equal(p, o) for p, o in zip(first, out))
