@@ -316,7 +316,8 @@ int mxq_mask_interval(const void* x, int dtype, size_t n, float lo, float hi, vo
  * Quantization.  The scale is the smallest power of two S >= 2^-127 with amax <= S * (largest element value): nothing is
  * clipped.  code = RNE(v / S); the quotient is exact.  A block that holds an infinity or a NaN gets the scale byte 0xFF and
  * codes 0x7F throughout: it reads back as NaN.  (These calls, unlike those above, take such inputs.)
- * De-quantization.  value(code) * S in binary32, then rounded to the output's type.
+ * De-quantization.  value(code) * S in binary32, then rounded to the output's type.  At the upper end of binary32 that may be an infinity: finite
+ * magnitudes from 1.9375 * 2^127 (E4M3) or 1.875 * 2^127 (E5M2) on are rounded to 2^128 by their code.
  * Arithmetic is binary32 unless said otherwise.  rows <= 2^31 - 1, at most 2^41 elements (rows padded to a multiple of
  * 128), MXQ_ERR_TOO_LARGE beyond.  Outputs overlap neither inputs nor one another, except where a call says so.
  * Aligned pieces of 16 bytes (4 for scale bytes) that hold a byte of an input are read whole.
@@ -335,7 +336,7 @@ int mxq_dequantize8(const uint8_t* d_codes, const uint8_t* d_scales, size_t rows
 /*
  * mxq_add_rmsnorm8 -- residual addition and root-mean-square norm with the output in 8 bits:
  *   h = x + residual, rounded to dtype (h = x without a residual)
- *   rstd = 1 / sqrt(mean(h^2) + eps)          per row
+ *   rstd = 1 / sqrt(mean(h^2) + eps)          per row; the sum of squares is binary32: where it passes 2^128, rstd and y are zeros
  *   y = (h * rstd) * weight                   -> out_codes, out_scales
  *   residual, out_sum   both or neither NULL.  out_sum receives h: the next residual.  It may be x or residual itself
  *                       (same stride), which is then updated in place.
@@ -373,7 +374,8 @@ int mxq_add_rmsnorm8_backward(const void* dy, const void* dsum, const void* weig
 
 /*
  * mxq_swiglu8 -- gated activation with the output in 8 bits: a = gate / (1 + exp(-gate)) * up -> out_codes, out_scales.
- * gate and up may be the two halves of one tensor's rows.
+ * gate and up may be the two halves of one tensor's rows.  A sigmoid 1 / (1 + exp(-gate)) below 2^-126 (gate < -87.3) counts as zero; here and in the
+ * gradient exp(-gate) is good to 4 * 2^-24 relative for fp32 tensors and to (1.3 |gate| + 4) * 2^-24 for bf16 ones.
  *   gate_codes, gate_scales, up_codes, up_scales   all or none NULL: gate and up in 8 bits, for mxq_swiglu8_backward.
  */
 int mxq_swiglu8(const void* gate, const void* up, int dtype, size_t rows, size_t cols, size_t gate_stride,

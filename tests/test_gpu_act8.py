@@ -750,3 +750,54 @@ def test_where_rows_start_changes_no_bit_that_is_elementwise(rows, cols, B, dtyp
         out = [t.t.clone() for t in wide] + [t.t.clone() for pair in (kept, q, act, gk, uk) for t in pair]
         first = first or out
         assert all(torch.equal(p, o) for p, o in zip(first, out))
+
+
+@pytest.mark.parametrize("fmt,first", [(ref.E4M3, 1.9375), (ref.E5M2, 1.875)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_upper_end_of_the_format(fmt, first, dtype):
+    """Finite magnitudes that a code rounds to 2^128 read back as infinities, the next smaller ones do not; neighbours in the block keep their values."""
+    below = first - (2.0 ** -7 if dtype == BF16 else 2.0 ** -23)
+    x = torch.zeros(4, 32, dtype=torch.float64)
+    for row, m in enumerate((first, below, -first, torch.finfo(dtype).max / 2.0 ** 127)):
+        x[row, 5], x[row, 6] = m * 2.0 ** 127, 2.0 ** 126
+    x = x.to(dtype).cuda()
+    c, s = mxq.quantize8(x, 32, fmt)
+    wc, ws = ref.quantize(np64(x), 32, fmt)
+    assert np.array_equal(c.view(torch.uint8).cpu().numpy(), wc) and np.array_equal(s.view(torch.uint8).cpu().numpy(), ws)
+    back = torch.empty_like(x)
+    mxq.mxq_dequantize8(c, s, 32, fmt, back)
+    inf = float("inf")
+    assert back[0, 5] == inf and torch.isfinite(back[1, 5]) and back[2, 5] == -inf and back[3, 5] == inf
+    assert bool((back[:, 6] == 2.0 ** 126).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("cols", [64, 1001, 2048])
+def test_a_sum_of_squares_past_binary32_gives_zeros(cols, dtype):
+    x = torch.randn(3, cols, device="cuda").to(dtype)
+    x[1] = 2.0 ** 64
+    w, rstd = torch.ones(cols, device="cuda"), torch.empty(3, device="cuda")
+    c, s = mxq.alloc_outputs8(3, cols, 16, ref.E4M3, "cuda")
+    mxq.mxq_add_rmsnorm8(x, None, w, 1e-5, 16, ref.E4M3, None, c, s, None, None, rstd)
+    c = c.view(torch.uint8)
+    assert rstd[1] == 0 and bool(((c[1] & 0x7F) == 0).all()) and bool((s.view(torch.uint8)[1] == 0).all())
+    assert bool((rstd[[0, 2]] > 0).all()) and bool(((c[[0, 2]] & 0x7F) != 0).any(1).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_sigmoids_at_the_lower_end_of_binary32(dtype):
+    """Zero below 2^-126, in the forward pass and in both gradients, and no NaN there."""
+    gate = torch.tensor([-80.0, -87.0, -87.5, -88.0, -89.0, -1000.0, -3e38, 0.0] * 4, device="cuda").to(dtype).view(2, 16)
+    up = torch.full_like(gate, 2.0 ** 100)
+    (c, s), g, u = (mxq.alloc_outputs8(2, 16, 16, ref.E4M3, "cuda") for _ in range(3))
+    mxq.mxq_swiglu8(gate, up, 16, ref.E4M3, c, s, *g, *u)
+    held = torch.empty_like(gate)
+    mxq.mxq_dequantize8(c, s, 16, ref.E4M3, held)
+    far = gate < -87.4
+    assert bool((held[far] == 0).all()) and bool((held[gate == -80.0] < 0).all())
+    # the gradients of such gates, each in a block of its own scale so that the codes hold them
+    for v in (-88.0, -1000.0, -3e38):
+        (gc, gs), (uc, us) = mxq.quantize8(torch.full((1, 16), v, device="cuda"), 16, ref.E4M3), mxq.quantize8(torch.ones(1, 16, device="cuda"), 16, ref.E4M3)
+        dy, dg, du = torch.ones(1, 16, device="cuda", dtype=dtype), torch.empty(1, 16, device="cuda", dtype=dtype), torch.empty(1, 16, device="cuda", dtype=dtype)
+        mxq.mxq_swiglu8_backward(dy, gc, gs, uc, us, 16, ref.E4M3, dg, du)
+        assert bool((dg == 0).all()) and bool((du == 0).all()), v
