@@ -366,6 +366,11 @@ def mxq_mask_interval(x, n, lo, hi, d_out, stream=None) -> None:
 _CODE_TYPE = {MXQ_E4M3: torch.float8_e4m3fn, MXQ_E5M2: torch.float8_e5m2}
 
 
+def _check_block8(block_size) -> None:
+    if isinstance(block_size, bool) or not isinstance(block_size, int) or block_size not in (16, 32, 64, 128):
+        raise MxqError(f"block_size must be 16, 32, 64 or 128, got {block_size}")
+
+
 class _Call8:
     """Checks the tensors of one call against each other; the first wide tensor gives rows, cols, type and device."""
 
@@ -376,8 +381,7 @@ class _Call8:
             raise MxqError("a tensor of rows is expected, got a scalar")
         if first.numel() == 0:
             raise MxqError(f"at least one row and one element a row are expected, got {tuple(first.shape)}")
-        if isinstance(block_size, bool) or not isinstance(block_size, int) or block_size not in (16, 32, 64, 128):
-            raise MxqError(f"block_size must be 16, 32, 64 or 128, got {block_size}")
+        _check_block8(block_size)
         self.device, self.dtype, self.elem_fmt = first.device, first.dtype, elem_fmt
         self.cols = first.shape[-1]
         self.rows = first.numel() // self.cols
@@ -488,6 +492,8 @@ def mxq_add_rmsnorm8_backward(dy, dsum, weight, kept_codes, kept_scales, rstd, b
     pw = c.vector(weight, "weight", c.cols, None)
     kept, prs = c.held(kept_codes, kept_scales, "kept_"), c.vector(rstd, "rstd", c.rows)
     pdw = c.vector(dweight, "dweight", c.cols, optional=True)
+    if d_workspace is not None:
+        c._on_device(d_workspace, "d_workspace")
     pws = c.vector(d_workspace, "d_workspace", d_workspace.numel(), None) if d_workspace is not None else 0
     ws_bytes = d_workspace.numel() * d_workspace.element_size() if d_workspace is not None else 0
     with torch.cuda.device(c.device):
@@ -578,6 +584,9 @@ def tensor_mse(block_sse: torch.Tensor, n: int, stream=None) -> torch.Tensor:
 
 def alloc_outputs8(rows: int, cols: int, block_size: int, elem_fmt: int, device):
     """Codes and scales of one 8-bit tensor, as the float8 types that torch has for them."""
+    _check_block8(block_size)
+    if elem_fmt not in _CODE_TYPE:
+        raise MxqError(f"elem_fmt must be MXQ_E4M3 or MXQ_E5M2, got {elem_fmt}")
     codes = torch.empty(rows, cols, dtype=_CODE_TYPE[elem_fmt], device=device)
     scales = torch.empty(rows, -(-cols // block_size), dtype=torch.float8_e8m0fnu, device=device)
     return codes, scales
@@ -585,7 +594,7 @@ def alloc_outputs8(rows: int, cols: int, block_size: int, elem_fmt: int, device)
 
 def quantize8(x: torch.Tensor, block_size: int = 32, elem_fmt: int = MXQ_E4M3, stream=None):
     """Allocates (codes, scales) and runs mxq_quantize8 on the rows of x."""
-    cols = x.shape[-1]
-    codes, scales = alloc_outputs8(x.numel() // cols if cols else 0, cols, block_size, elem_fmt, x.device)
+    c = _Call8(x, block_size, elem_fmt)
+    codes, scales = alloc_outputs8(c.rows, c.cols, block_size, elem_fmt, c.device)
     mxq_quantize8(x, block_size, elem_fmt, codes, scales, stream)
     return codes, scales

@@ -99,6 +99,19 @@ def test_binding_refuses_what_is_not_on_a_gpu(lib):
             f()
 
 
+def test_helpers_refuse_options_that_there_are_not(lib):
+    from paper_2605_08565_b200 import binding as mxq
+    for B in (0, 8, 24, -32, 32.0, True, None):
+        with pytest.raises(mxq.MxqError, match="block_size"):
+            mxq.alloc_outputs8(4, 64, B, mxq.MXQ_E4M3, "cpu")
+    for fmt in (2, -1, None):
+        with pytest.raises(mxq.MxqError, match="elem_fmt"):
+            mxq.alloc_outputs8(4, 64, 32, fmt, "cpu")
+    for x in (torch.tensor(1.0), None, 3):
+        with pytest.raises(mxq.MxqError, match="CUDA tensors only"):
+            mxq.quantize8(x)
+
+
 @pytest.mark.parametrize("fmt,kind", [(ref.E4M3, torch.float8_e4m3fn), (ref.E5M2, torch.float8_e5m2)])
 def test_reference_formats_and_rounding_are_torch_s(fmt, kind):
     codes = np.arange(256, dtype=np.uint8)

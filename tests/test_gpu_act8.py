@@ -801,3 +801,18 @@ def test_sigmoids_at_the_lower_end_of_binary32(dtype):
         dy, dg, du = torch.ones(1, 16, device="cuda", dtype=dtype), torch.empty(1, 16, device="cuda", dtype=dtype), torch.empty(1, 16, device="cuda", dtype=dtype)
         mxq.mxq_swiglu8_backward(dy, gc, gs, uc, us, 16, ref.E4M3, dg, du)
         assert bool((dg == 0).all()) and bool((du == 0).all()), v
+
+
+def test_helpers_and_workspaces_that_do_not_fit_are_refused(route):
+    x = torch.zeros(4, 64, device="cuda", dtype=BF16)
+    u8 = lambda *n: torch.zeros(*n, device="cuda", dtype=torch.uint8)  # noqa: E731
+    c, s, w, f = u8(4, 64), u8(4, 2), torch.ones(64, device="cuda"), torch.ones(4, device="cuda")
+    back = lambda ws: mxq.mxq_add_rmsnorm8_backward(x, None, w, c, s, f, 32, 0, x.clone(), w.clone(), ws)  # noqa: E731
+    back(torch.empty(256, device="cuda"))
+    for f_, text in ((lambda: mxq.quantize8(x, 0), "block_size"), (lambda: mxq.quantize8(x, 24), "block_size"), (lambda: mxq.quantize8(x, 32, 2), "elem_fmt"),
+                     (lambda: mxq.quantize8(x[0, 0]), "scalar"), (lambda: mxq.quantize8(x[:, :0]), "at least one"), (lambda: mxq.quantize8(x[:0]), "at least one"),
+                     (lambda: back(torch.empty(256)), "CUDA tensors only"), (lambda: back(4096), "CUDA tensors only"),
+                     (lambda: back(torch.empty(512, device="cuda")[::2]), "contiguous"), (lambda: back(torch.empty(255, device="cuda")), "status 6"),
+                     (lambda: back(torch.empty(300, device="cuda")[1:]), "status 4")):
+        with pytest.raises(mxq.MxqError, match=text):
+            f_()
