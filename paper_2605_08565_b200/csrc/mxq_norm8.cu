@@ -14,6 +14,14 @@ struct NormShape {
     int lanes_log2, group;
 };
 
+// A vector's part of the weight's gradient, in the kernels that stream rows of whole vectors: 32 bytes at a time where the workspace starts on 32 bytes, else 16
+// (8192 x 4096 bf16 42.3 us, and 43.1 with 16 throughout).
+template <int V>
+__device__ __forceinline__ void store_parts(float* parts, size_t at, const Place& t, const float (&v)[V]) {
+    if ((reinterpret_cast<uintptr_t>(parts) & 31u) == 0) store_wide<kF32, kWhole>(parts, at, t, v);
+    else store_wide<kF32, kHalf>(parts, at, t, v);
+}
+
 // Sum over the CTA, the same bits in every thread.  sums: T / 32 floats, those of warps that the CTA does not have zeros, which nothing else
 // uses between the barrier inside and the next one.
 template <int T>
@@ -104,11 +112,13 @@ __global__ void __launch_bounds__(T, T == 512 ? 3 : 1) k_add_rmsnorm8(const void
 }
 
 // A CTA takes every gridDim.x-th row (or group of rows); a thread holds the same K vectors of each and adds up its columns' part of the
-// weight's gradient.  The parts (here and in the kernels below) are stored 16 bytes at a time, which every workspace allows: its address has no say
-// in which kernel runs, so that dx and dweight are the same bits with any workspace.
+// weight's gradient.  The workspace's address has no say in which kernel runs (here and below), only in how wide the parts are stored, so that
+// dx and dweight are the same bits with any workspace.
 // Registers for two CTAs of 512 threads an SM: 8192 x 4101 bf16 146 us with one, 100 with two (8192 x 4104: 101, 58); limiting those of 256 threads to
 // three an SM costs 0 to 20 %.
-template <int DT, int FMT, int FIT, int K, bool SMALL, int T>
+// PARTS: how the parts are stored, FIT or, of whole rows in a workspace that does not start on 32 bytes, kHalf.  (Both in one kernel, behind a branch, cost registers:
+// 2048 x 32768 bf16 269 us like this and 373, fp32 391 and 422.)
+template <int DT, int FMT, int FIT, int PARTS, int K, bool SMALL, int T>
 __global__ void __launch_bounds__(T, T == 512 ? 2 : 1) k_add_rmsnorm8_backward(const void* dy, size_t dy_stride, const void* dsum, size_t ds_stride, const void* weight,
                                                                               int weight_dtype, Held8 kept, const float* rstd, float inv_cols, NormShape n, void* dx, size_t dx_stride,
                                                                               float* parts) {
@@ -192,14 +202,15 @@ __global__ void __launch_bounds__(T, T == 512 ? 2 : 1) k_add_rmsnorm8_backward(c
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const Place t = place_of<V, SMALL>(n, 0, k);
-            store_wide<kF32, FIT == kAny ? kAny : kHalf>(parts, blockIdx.x * n.cols + t.vec * V, t, dw[k]);
+            store_wide<kF32, PARTS>(parts, blockIdx.x * n.cols + t.vec * V, t, dw[k]);
         }
     }
 }
 
 // ---- rows of whole vectors, one vector a thread ------------------------------------------------------------------------------------
 // A CTA takes every gridDim.x-th row and copies the next one into shared memory while it works on the present one, so that what is under way
-// from memory does not depend on the threads' registers, nor stop while the CTA meets in its barrier.  T: the most threads of a CTA.
+// from memory does not depend on the threads' registers, nor stop while the CTA meets in its barrier.  T: the most threads of a CTA.  Only where the weight's
+// vectors are as aligned as the rows: 8192 x 4096 bf16 gradient 43 us, and 62 with a weight on 16 bytes, 83 on 2 (norm 43, 48, 63), from the kernels above.
 
 // The 32 vectors of a warp: each lane copies two of their 64 pieces of 16 bytes, 512 bytes apart, so that an instruction asks for whole
 // sectors (each lane its own two pieces: twice the requests to L2).  Piece p lies at p ^ (p >> 3 & 1), without which the lanes' reads of every
@@ -314,8 +325,9 @@ __global__ void __launch_bounds__(T, T == 256 ? (RES ? 2 : 4) : T <= 384 ? (RES 
 // that is loaded one row ahead has to arrive within that row, because the loop's end moves it (8192 x 4096: 62 us, and 47 like this).
 constexpr int kMeta = 12;   // 32 bytes off the grid lie in 9 words; rstd; 2 unused
 
-// 117 registers: two CTAs of up to 320 threads an SM (8192 x 5120 62.5 us with one, 51.4 with two).  Limited to what a third one, or a second
-// one of 384 threads, leaves, the compiler spills (8192 x 4096 41.9 -> 62.4, 8192 x 6144 68.8 -> 88.8).
+// bf16: 126 to 128 registers a thread at 256 threads and 96 at 320, which its bound asks for: two CTAs an SM (8192 x 5120 62.5 us with one, 51.4 with
+// two); 142 to 150 at 384 and 128 at 512: one.  fp32: 96 to 114, 64 at 1024 threads.  Limited to what a third CTA of 256 threads, or a second
+// one of 384, leaves, the compiler spills (8192 x 4096 41.9 -> 62.4, 8192 x 6144 68.8 -> 88.8).
 template <int DT, int FMT, bool DSUM, int T>
 __global__ void __launch_bounds__(T, T <= 320 ? 2 : 1)
     k_add_rmsnorm8_backward_rows(const char* dy, size_t dy_step, const char* dsum, size_t ds_step, const void* weight, int weight_dtype, Held8 kept, const float* rstd,
@@ -413,7 +425,7 @@ __global__ void __launch_bounds__(T, T <= 320 ? 2 : 1)
         slot = other;
         other = done;
     }
-    if (parts) store_wide<kF32, kHalf>(parts, blockIdx.x * n.cols + t.vec * V, t, dw);
+    if (parts) store_parts(parts, blockIdx.x * n.cols + t.vec * V, t, dw);
 }
 
 // The same for rows of 8193 to 16384 bf16 elements: 512 threads of two vectors.  Nothing but the weight's gradient is kept in registers; dy and the codes
@@ -531,7 +543,7 @@ __global__ void __launch_bounds__(512, 1)
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const Place t = place_of<V, false>(n, 0, k);
-        store_wide<kF32, kHalf>(parts, blockIdx.x * n.cols + t.vec * V, t, dw[k]);
+        store_parts(parts, blockIdx.x * n.cols + t.vec * V, t, dw[k]);
     }
 }
 
@@ -723,7 +735,10 @@ cudaError_t launch_add_rmsnorm8_backward(const Wide8& dy, const Wide8& dsum, con
     } else {
         err = pick(dtype, fmt, fit, l, [&](auto dt, auto fm, auto v, auto k, auto small, auto threads) {
             static std::atomic<int> cache[33][kMaxDevices];
-            auto* kernel = k_add_rmsnorm8_backward<dt(), fm(), v(), k(), small(), threads()>;
+            auto* kernel = k_add_rmsnorm8_backward<dt(), fm(), v(), v(), k(), small(), threads()>;
+            if constexpr (v() == kWhole && !small()) {   // 1024 threads either way: one CTA an SM, the same split of the rows
+                if (reinterpret_cast<uintptr_t>(parts) & 31u) kernel = k_add_rmsnorm8_backward<dt(), fm(), v(), kHalf, k(), small(), threads()>;
+            }
             cudaError_t e = rows_grid((const void*)kernel, 0, 0, l.threads, cache, (rows + l.rows_cta - 1) / l.rows_cta, kNorm8Parts, grid);
             if (e != cudaSuccess) return e;
             count_launch();
