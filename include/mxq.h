@@ -308,8 +308,9 @@ int mxq_mask_interval(const void* x, int dtype, size_t n, float lo, float hi, vo
  * Layout.  rows x cols elements; a block is block_size (16, 32, 64 or 128) consecutive elements of a ROW, the last
  * one of a row may be short.
  *   wide tensors   x, residual, dy, ...: MXQ_F32 or MXQ_BF16, rows *_stride elements apart (>= cols), elements of a row
- *                  contiguous; aligned to their element.  Rows that start on 16 bytes and hold a multiple of 8 elements
- *                  are read and written 16 bytes at a time, others element by element.
+ *                  contiguous; aligned to their element.  Rows that start on 32 bytes and hold a multiple of 32 bytes move 32 bytes at a
+ *                  time; on 16 bytes and of a multiple of 16, in halves; all others in aligned 16-byte pieces that are shifted into place.
+ *                  The least of a call's wide tensors (for the norms, and their weight, too) decides for all of them.
  *   codes          rows * cols bytes, one element each: E4M3 (bias 7, largest 448, 0x7F and 0xFF NaN) or E5M2 (bias 15,
  *                  largest 57344).  16-byte aligned.
  *   scales         rows * ceil(cols / block_size) bytes, UE8M0: 2^(byte - 127); 0xFF is NaN.  Any alignment.

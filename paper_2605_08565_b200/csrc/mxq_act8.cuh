@@ -8,7 +8,7 @@
 // How rows lie (FIT): kWhole, they start on 32 bytes and hold whole vectors, which are read and written at once; kHalf, the same of 16 bytes
 // and half vectors; kAny, all others (an odd number of elements, a view that starts anywhere).  Those are read in the aligned 16-byte
 // pieces that their bytes lie in, shifted into place in registers; on the way out neighbouring lanes exchange what belongs into the
-// other's aligned pieces, and only the two ends of a warp's run are stored element by element.
+// other's aligned pieces, and only the two ends of a warp's run of a row are stored in pieces of 1 to 8 bytes.
 #pragma once
 
 #include <cuda_bf16.h>
