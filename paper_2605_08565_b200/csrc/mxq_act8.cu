@@ -82,8 +82,9 @@ __device__ __forceinline__ float2 sigmoid2(float2 g) {
     return r;
 }
 
-// Registers for five (six) CTAs an SM: 8192 x 14336 with the checkpoints 129 us (four 132, six 140), without 93 with five or six (four 100): a few passes in
-// a row, as all figures here; a tenth of a second of them draws the power limit and takes 139 and 103.  Shifted bf16 rows, 8192 x 3075: with the checkpoints four, 55 (one 63, five 60), without six, 32 (one 38, five 35).
+// Registers for five (six) CTAs an SM: 8192 x 14336 with the checkpoints 129 us (four 132, six 140), without 93 with five or six (four 100), in a few passes
+// one after the other, like the figures below; a tenth of a second of them meets the power limit and takes 139 and 103.  Shifted bf16 rows, 8192 x 3075: with
+// the checkpoints four, 55 (one 63, five 60), without six, 32 (one 38, five 35).
 template <int DT, int FMT, int FIT, bool KEEP>
 __global__ void __launch_bounds__(kThreads, KEEP ? (FIT == kAny ? 4 : 5) : 6) k_swiglu8(const void* gate, size_t gate_stride, const void* up, size_t up_stride, Rows8 r, Held8 out, Held8 out_gate, Held8 out_up) {
     constexpr int V = vec_elems(DT);
