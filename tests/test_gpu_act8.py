@@ -816,3 +816,80 @@ def test_helpers_and_workspaces_that_do_not_fit_are_refused(route):
                      (lambda: back(torch.empty(300, device="cuda")[1:]), "status 4")):
         with pytest.raises(mxq.MxqError, match=text):
             f_()
+
+
+@pytest.fixture
+def memory_given_back():
+    yield
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("cols", [4096, 4097])
+def test_tensors_of_more_than_32_bits_of_elements(cols, memory_given_back):
+    """2^32 elements and some rows: the first and the last rows are the bits that calls on those rows alone give."""
+    rows, B, fmt, few = (1 << 20) + 70, 32, ref.E4M3, 64
+    if torch.cuda.mem_get_info()[0] < (60 << 30):
+        pytest.skip("not enough free memory")
+    x, r = (torch.empty(rows, cols, dtype=BF16, device="cuda").normal_() for _ in range(2))
+    x0, r0 = ([t[:few].clone(), t[-few:].clone()] for t in (x, r))
+    w = torch.linspace(0.5, 1.5, cols, device="cuda")
+    y, kept, rstd = mxq.alloc_outputs8(rows, cols, B, fmt, "cuda"), mxq.alloc_outputs8(rows, cols, B, fmt, "cuda"), torch.empty(rows, device="cuda")
+    ends = lambda *ts: [[t[:few].clone().view(torch.uint8) if t.element_size() == 1 else t[:few].clone() for t in ts],  # noqa: E731
+                        [t[-few:].clone().view(torch.uint8) if t.element_size() == 1 else t[-few:].clone() for t in ts]]
+
+    def same(got, want):
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+    mxq.mxq_add_rmsnorm8(x, r, w, 1e-5, B, fmt, r, *y, *kept, rstd)
+    got = ends(r, *y, *kept, rstd)
+    for k in (0, 1):
+        y1, k1, s1, h1 = mxq.alloc_outputs8(few, cols, B, fmt, "cuda"), mxq.alloc_outputs8(few, cols, B, fmt, "cuda"), torch.empty(few, device="cuda"), torch.empty_like(x0[k])
+        mxq.mxq_add_rmsnorm8(x0[k], r0[k], w, 1e-5, B, fmt, h1, *y1, *k1, s1)
+        same(got[k], [h1] + [t.view(torch.uint8) for t in (*y1, *k1)] + [s1])
+    # the gradient with x as dy and the sum as dsum, over x
+    r1 = [got[k][0] for k in (0, 1)]
+    mxq.mxq_add_rmsnorm8_backward(x, r, w, *kept, rstd, B, fmt, x)
+    got = ends(x)
+    for k in (0, 1):
+        k1 = [(t[:few] if k == 0 else t[-few:]).clone() for t in kept]
+        s1, d1 = (rstd[:few] if k == 0 else rstd[-few:]).clone(), torch.empty_like(x0[k])
+        mxq.mxq_add_rmsnorm8_backward(x0[k], r1[k], w, *k1, s1, B, fmt, d1)
+        same(got[k], [d1])
+    x1 = [got[k][0] for k in (0, 1)]
+    # the gated activation of (x, r) with its gradient, store and load
+    mxq.mxq_swiglu8(x, r, B, fmt, *y, *kept, *(u := mxq.alloc_outputs8(rows, cols, B, fmt, "cuda")))
+    got = ends(*y, *kept, *u)
+    held = []
+    for k in (0, 1):
+        a = [mxq.alloc_outputs8(few, cols, B, fmt, "cuda") for _ in range(3)]
+        mxq.mxq_swiglu8(x1[k], r1[k], B, fmt, *a[0], *a[1], *a[2])
+        same(got[k], [t.view(torch.uint8) for p in a for t in p])
+        held.append(a)
+    other = torch.empty_like(x)
+    mxq.mxq_swiglu8_backward(x, *kept, *u, B, fmt, x, other)
+    got = ends(x, other)
+    for k in (0, 1):
+        dg, du = torch.empty_like(x1[k]), torch.empty_like(x1[k])
+        mxq.mxq_swiglu8_backward(x1[k], *held[k][1], *held[k][2], B, fmt, dg, du)
+        same(got[k], [dg, du])
+    mxq.mxq_quantize8(r, B, fmt, *y)
+    mxq.mxq_dequantize8(*y, B, fmt, other)
+    got = ends(*y, other)
+    for k in (0, 1):
+        c1, s1 = mxq.quantize8(r1[k], B, fmt)
+        back = torch.empty_like(r1[k])
+        mxq.mxq_dequantize8(c1, s1, B, fmt, back)
+        same(got[k], [c1.view(torch.uint8), s1.view(torch.uint8), back])
+
+
+def test_rows_times_lanes_past_32_bits(memory_given_back):
+    """Rows of one element in blocks of 128: 2^32 vectors and some, most of them behind the ends of the rows."""
+    rows, few = (1 << 29) + 7, 1000
+    x = torch.empty(rows, 1, dtype=BF16, device="cuda").normal_()
+    c, s = mxq.quantize8(x, 128, ref.E5M2)
+    back = torch.empty_like(x)
+    mxq.mxq_dequantize8(c, s, 128, ref.E5M2, back)
+    for part in (slice(0, few), slice(rows // 2, rows // 2 + few), slice(rows - few, rows)):
+        wc, ws = ref.quantize(np64(x[part]), 128, ref.E5M2)
+        assert np.array_equal(c[part].view(torch.uint8).cpu().numpy(), wc) and np.array_equal(s[part].view(torch.uint8).cpu().numpy(), ws)
+        assert np.array_equal(np64(back[part]), ref.dequantize(wc, ws, 128, ref.E5M2))
